@@ -128,7 +128,8 @@ def _run_own(s):
             return dict(out=out, normed=normed)
         stats = sq.residual_norm_stats(s["x"])
         out, normed = sq.residual_norm(s["x"], s["y"], s["z"], *w, eps=EPS, stats=stats)
-        dx, dy, dz, dpost, dscale, dpre = sq.residual_norm_backward(s["grad_out"], s["grad_normed"], s["x"], s["y"], s["z"], *w, stats)
+        dx, dy, dz, dpost, dscale, dpre = sq.residual_norm_backward(s["grad_out"], s["grad_normed"], s["x"], s["y"], s["z"], *w, stats,
+                                                                  eps=EPS)
         return dict(out=out, normed=normed, dx=dx, dy=dy, dz=dz, dpost=dpost, dscale=dscale, dpre=dpre)
     if not s["train"]:
         y, state = sq.gated_scan(s["x"], s["r"], s["g"], s["rate"], s["state"], s["lengths"])
