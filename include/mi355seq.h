@@ -1,0 +1,186 @@
+/*
+ * mi355seq.h -- C ABI of the sequence operators for MI355X (gfx950): the gated
+ * linear recurrence along the tokens, and the norms before and after a block
+ * with its gate and scaled residual, each with its gradient.
+ *
+ * A time-invariant filter along a long axis is a convolution, which the FFT
+ * plans of mi355fft.h compute; these operators are what stands beside it in a
+ * sequence-mixing block: a filter whose coefficients the data set token by
+ * token, and the element-wise ends of the block.
+ *
+ * Conventions shared by every entry point
+ *   - Activations are FP32, FP16 or BF16, all of one call in the same type;
+ *     weights, states, statistics and weights' gradients are FP32.  Arithmetic
+ *     is FP32; an activation is rounded once, when it is written.
+ *   - Sizes and strides count elements.  Channels are consecutive in memory;
+ *     the other axes have any stride (inputs also 0).  Pointers are aligned to
+ *     one element.
+ *   - Every pointer argument but `strides` is a DEVICE pointer on the current
+ *     HIP device; the caller owns it.  A workspace is scratch memory of one
+ *     call: it needs no initial contents, and no other call may use it at the
+ *     same time.
+ *   - Every call is stream-ordered on the given hipStream_t (0 = the null
+ *     stream), never synchronises and allocates nothing, so it can be captured
+ *     into a graph.  Argument errors are returned before any HIP call is made.
+ *   - Results do not depend on timing: two calls on the same inputs give the
+ *     same bits.
+ */
+#ifndef MI355SEQ_H
+#define MI355SEQ_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include <hip/hip_runtime_api.h>
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Types of the activations. */
+enum { SEQ_FP32 = 0, SEQ_FP16 = 1, SEQ_BF16 = 2 };
+
+/* Return codes: the values of mi355fft.h. */
+enum {
+    SEQ_OK = 0,
+    SEQ_EINVAL = -1,       /* invalid argument (NULL, bad enum, overlapping buffers) */
+    SEQ_EUNSUPPORTED = -2, /* valid request this library does not implement (size) */
+    SEQ_EALIGN = -4,       /* a pointer is not aligned to one element (workspace: 16 bytes) */
+    SEQ_EHIP = -5          /* the HIP runtime reported an error */
+};
+
+/* Tokens between the states that seq_scan_forward saves for the gradient. */
+enum { SEQ_SCAN_CHUNK = 16 };
+
+/*
+ * seq_scan_forward -- the gated linear recurrence of each channel.
+ *
+ *     q_t = rate * s(r_t),  c_t = s(g_t) * x_t,  s(v) = 1 / (1 + exp(-v))
+ *     h_t = h_(t-1) + q_t * (c_t - h_(t-1)),  y_t = h_t
+ *
+ * for t = 0 .. n-1, with h_(-1) the given state.  q_t = 0 keeps the state,
+ * q_t = 1 replaces it; a rate in (0, 1] bounds q_t (the range is not checked).
+ *
+ *   batch, len   sequences (>= 0) and tokens of each (>= 0); len = 1 is the
+ *                single-token step of a server.
+ *   channels     >= 1.  batch, len and channels are at most 2^31 - 1, their
+ *                product at most 2^40 (else SEQ_EUNSUPPORTED).
+ *   type         SEQ_FP32, SEQ_FP16 or SEQ_BF16: x, r, g and y.
+ *   x, r, g      inputs (batch, len, channels).
+ *   strides      host array of 8: batch and token stride of x, r, g, y; NULL:
+ *                all contiguous.  The rows of y must not overlap each other.
+ *   rate         (channels) FP32.
+ *   state        (batch, channels) FP32, contiguous; NULL: zeros.
+ *   lengths      (batch) int32: the tokens of each sequence that count, taken
+ *                as 0 below 0 and as len beyond it; NULL: all.  Tokens behind
+ *                them leave the state as it is, whatever their values (NaN
+ *                included), and have y = 0.
+ *   y            output; may be x, r or g itself with the same strides,
+ *                otherwise must not share elements with an input.
+ *   state_out    (batch, channels) FP32 or NULL: the state after the last
+ *                token that counts; may be `state` itself.
+ *   saved        NULL, or seq_scan_saved_bytes() for the gradient: the state
+ *                before every 16th token, (batch, ceil(len / 16), channels).
+ *   workspace    seq_scan_workspace_bytes(.., 0) bytes, aligned to 16; may be
+ *                NULL where that is 0.
+ * Returns SEQ_OK, SEQ_EINVAL, SEQ_EUNSUPPORTED, SEQ_EALIGN or SEQ_EHIP.
+ */
+int seq_scan_forward(int64_t batch, int64_t len, int64_t channels, int type, const void *x, const void *r,
+                     const void *g, const int64_t *strides, const float *rate, const float *state,
+                     const int32_t *lengths, void *y, float *state_out, float *saved, void *workspace,
+                     hipStream_t stream);
+
+/*
+ * seq_scan_backward -- the gradient of seq_scan_forward.
+ *
+ * With d_t the gradient that reaches h_t,
+ *     d_t = dy_t + k_(t+1),  k_t = (1 - q_t) d_t,  e_t = d_t (c_t - h_(t-1))
+ *     dx_t = d_t q_t s(g_t),  dg_t = dx_t x_t (1 - s(g_t))
+ *     dr_t = e_t q_t (1 - s(r_t)),  drate = sum over batch and tokens of e_t s(r_t)
+ * and k behind the last token that counts the gradient of state_out.  The
+ * states h are computed again in FP32 from `saved`.
+ *
+ *   dy           gradient of y (batch, len, channels).
+ *   strides      host array of 14: batch and token stride of dy, x, r, g, dx,
+ *                dr, dg; NULL: all contiguous.
+ *   saved        as written by seq_scan_forward on the same inputs.
+ *   dstate_out   gradient of state_out, (batch, channels) FP32; NULL: zeros.
+ *   dx, dr, dg   outputs; 0 at tokens that do not count.  They may be slices
+ *                of one buffer; no output may share elements with an input
+ *                (dx may be dy, dr may be r, dg may be g, with the same
+ *                strides).
+ *   drate        (channels) FP32 output.
+ *   dstate       (batch, channels) FP32 or NULL: gradient of `state`.
+ *   workspace    seq_scan_workspace_bytes(.., 1) bytes, aligned to 16.
+ */
+int seq_scan_backward(int64_t batch, int64_t len, int64_t channels, int type, const void *dy, const void *x,
+                      const void *r, const void *g, const int64_t *strides, const float *rate, const float *saved,
+                      const int32_t *lengths, const float *dstate_out, void *dx, void *dr, void *dg, float *drate,
+                      float *dstate, void *workspace, hipStream_t stream);
+
+/* Bytes of `saved` and of the workspace of the forward (0) or backward (1)
+ * call; 0 also for an invalid or unsupported request. */
+size_t seq_scan_saved_bytes(int64_t batch, int64_t len, int64_t channels);
+size_t seq_scan_workspace_bytes(int64_t batch, int64_t len, int64_t channels, int type, int backward);
+
+/*
+ * seq_norm_forward -- the end of a block and the beginning of the next one:
+ *
+ *     o = x + scale * post * (y / rms(y)) * (z s(z)),  n = pre * o / rms(o)
+ *     rms(v) = sqrt(mean of v^2 over the row + eps)
+ *
+ *   rows, channels  rows >= 0, channels in [1, 65536] (else SEQ_EUNSUPPORTED).
+ *   x            the residual stream (rows, channels).
+ *   y            the block's output, normalised; NULL: no block (the first norm
+ *                of a model: o = x), then z, post, scale and out are NULL too.
+ *   z            the gate; NULL: none.
+ *   strides      host array of 5: row stride of x, y, z, out, normed; NULL:
+ *                contiguous.
+ *   post, scale, pre  (channels) FP32.  scale NULL: 1.  pre NULL: no second
+ *                norm, then normed is NULL too.
+ *   eps          > 0.
+ *   out          o; may be x itself with the same stride.
+ *   normed       n, from o before it is rounded; may be y or z itself with the
+ *                same stride.
+ *   stats        NULL, or (rows, 2) FP32 for the gradient: 1 / rms(y) and
+ *                1 / rms(o) of each row (the one that does not occur is 0).
+ */
+int seq_norm_forward(int64_t rows, int64_t channels, int type, const void *x, const void *y, const void *z,
+                     const int64_t *strides, const float *post, const float *scale, const float *pre, float eps,
+                     void *out, void *normed, float *stats, hipStream_t stream);
+
+/*
+ * seq_norm_backward -- the gradient of seq_norm_forward.  With m = y / rms(y),
+ * oh = o / rms(o), v = dnormed * pre and G = z s(z):
+ *
+ *     t = dout + (v - oh mean(v oh)) / rms(o),  dx = t,  dpre = sum of dnormed oh
+ *     u = t scale post G,  dy = (u - m mean(u m)) / rms(y)
+ *     dz = t scale post m G'(z),  dscale = post P,  dpost = scale P,  P = sum of t G m
+ *
+ * sums over the rows in a fixed order.  With one channel v - oh mean(v oh)
+ * and u - m mean(u m) are taken as eps v / rms(o)^2 and eps u / rms(y)^2, which
+ * they equal: nothing would be left of the difference in FP32.
+ *
+ *   eps          as in the forward call.
+ *   dout, dnormed  gradients of o and n; dout NULL: 0; dnormed NULL where pre is.
+ *   strides      host array of 8: row stride of dout, dnormed, x, y, z, dx,
+ *                dy, dz; NULL: contiguous.
+ *   dx, dy, dz   outputs; dy and dz NULL where y and z are.  dx may be dout or
+ *                x, dy may be y or dnormed, dz may be z, with the same stride.
+ *   dpost, dscale, dpre  (channels) FP32 outputs; NULL where the weight is.
+ *   workspace    seq_norm_workspace_bytes() bytes, aligned to 16.
+ */
+int seq_norm_backward(int64_t rows, int64_t channels, int type, const void *dout, const void *dnormed,
+                      const void *x, const void *y, const void *z, const int64_t *strides, const float *post,
+                      const float *scale, const float *pre, float eps, const float *stats, void *dx, void *dy,
+                      void *dz, float *dpost, float *dscale, float *dpre, void *workspace, hipStream_t stream);
+
+size_t seq_norm_workspace_bytes(int64_t rows, int64_t channels, int type);
+
+/* English text of a return code. */
+const char *seq_strerror(int code);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* MI355SEQ_H */

@@ -1,4 +1,4 @@
-"""Build libmi355fft.so (HIP, gfx950) in-tree with hipcc.
+"""Build libmi355fft.so and libmi355seq.so (HIP, gfx950) in-tree with hipcc.
 
 Every translation unit is compiled for gfx950 only, with packed-FP32 VALU
 instructions disabled (``-target-feature -packed-fp32-ops``); the host pass
@@ -31,6 +31,9 @@ SOURCES = ["fft_small.hip", "fft_n1024.hip", "fft_n2048.hip", "fft_n4096.hip", "
 # the FFT library neither links nor calls
 MEMBENCH_SOURCES = ["membench.hip"]
 MEMBENCH_LIB = os.path.join(PKG, "libmi355membench.so")
+# the sequence operators (include/mi355seq.h): a library of their own too
+SEQ_SOURCES = ["seq_scan.hip", "seq_norm.hip"]
+SEQ_LIB = os.path.join(PKG, "libmi355seq.so")
 
 
 def _compile(src: str) -> str:
@@ -59,15 +62,15 @@ def build(jobs: int | None = None, verbose: bool = True) -> str:
     """Compile every source and link the shared libraries; returns the FFT
     library's path."""
     os.makedirs(OBJ_DIR, exist_ok=True)
-    srcs = SOURCES + MEMBENCH_SOURCES
+    libs = {LIB: SOURCES, MEMBENCH_LIB: MEMBENCH_SOURCES, SEQ_LIB: SEQ_SOURCES}
+    srcs = [s for of_lib in libs.values() for s in of_lib]
     jobs = jobs or min(len(srcs), max(1, (os.cpu_count() or 1)), 8)
     with ThreadPoolExecutor(jobs) as ex:
-        objs = list(ex.map(_compile, srcs))
-    _link(objs[:len(SOURCES)], LIB)
-    _link(objs[len(SOURCES):], MEMBENCH_LIB)
-    if verbose:
-        print(f"built {LIB}")
-        print(f"built {MEMBENCH_LIB}")
+        objs = dict(zip(srcs, ex.map(_compile, srcs)))
+    for lib, of_lib in libs.items():
+        _link([objs[s] for s in of_lib], lib)
+        if verbose:
+            print(f"built {lib}")
     return LIB
 
 

@@ -1,0 +1,231 @@
+"""Host-side checks of the sequence operators' C ABI and their tensor functions:
+symbols, refusals, sizes, and the reference's own gradient.
+
+None of these make a compute call, so they run without a GPU: every argument
+error is returned before the library touches the HIP runtime.
+"""
+import os
+import re
+import subprocess
+
+import pytest
+import torch
+
+import seq_reference as ref
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "mi355seq.h")
+P = 1 << 40  # addresses that are never read, far apart
+GAP = 1 << 32
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2609_32237_amd import _seq_lib
+
+    return _seq_lib
+
+
+def declared_functions():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    return sorted(set(re.findall(r"\b([a-z_][a-z0-9_]*)\s*\([^;{]*\)\s*;", text)))
+
+
+def test_library_exports_what_the_header_declares(L):
+    out = subprocess.run(["nm", "-D", "--defined-only", L.LIB_PATH], capture_output=True, text=True, check=True).stdout
+    exported = set(re.findall(r" T (\w+)$", out, flags=re.M))
+    assert set(L.EXPORTS) == set(declared_functions()) <= exported
+
+
+def test_header_compiles_as_c():
+    src = f'#include "{HEADER}"\nint main(void) {{ return SEQ_OK; }}\n'
+    res = subprocess.run(["gcc", "-x", "c", "-std=c11", "-fsyntax-only", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-"],
+                         input=src, capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+
+
+def test_strerror_and_codes(L):
+    from paper_2609_32237_amd import _lib
+
+    codes = [L.SEQ_OK, L.SEQ_EINVAL, L.SEQ_EUNSUPPORTED, L.SEQ_EALIGN, L.SEQ_EHIP]
+    assert codes == [_lib.FFT_OK, _lib.FFT_EINVAL, _lib.FFT_EUNSUPPORTED, _lib.FFT_EALIGN, _lib.FFT_EHIP]
+    assert len({L.seq_strerror(c) for c in codes}) == len(codes)
+    assert L.seq_strerror(12345) == "unknown error code"
+
+
+def scan(L, **k):
+    a = dict(batch=2, len=100, channels=64, type=L.SEQ_BF16, x=P, r=P + GAP, g=P + 2 * GAP, strides=None, rate=P + 3 * GAP,
+             state=P + 4 * GAP, lengths=None, y=P + 5 * GAP, state_out=P + 6 * GAP, saved=P + 7 * GAP, workspace=P + 8 * GAP, stream=None)
+    a.update(k)
+    if a["strides"] is not None:
+        a["strides"] = L.int64s(a["strides"])
+    return L.lib.seq_scan_forward(*a.values())
+
+
+def scan_back(L, **k):
+    a = dict(batch=2, len=100, channels=64, type=L.SEQ_BF16, dy=P, x=P + GAP, r=P + 2 * GAP, g=P + 3 * GAP, strides=None,
+             rate=P + 4 * GAP, saved=P + 5 * GAP, lengths=None, dstate_out=P + 6 * GAP, dx=P + 7 * GAP, dr=P + 8 * GAP,
+             dg=P + 9 * GAP, drate=P + 10 * GAP, dstate=P + 11 * GAP, workspace=P + 12 * GAP, stream=None)
+    a.update(k)
+    if a["strides"] is not None:
+        a["strides"] = L.int64s(a["strides"])
+    return L.lib.seq_scan_backward(*a.values())
+
+
+ROW = 100 * 64
+PLAIN = [ROW, 64] * 4
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(batch=-1), "SEQ_EINVAL"), (dict(len=-1), "SEQ_EINVAL"), (dict(channels=0), "SEQ_EINVAL"), (dict(type=3), "SEQ_EINVAL"),
+    (dict(type=-1), "SEQ_EINVAL"), (dict(batch=1 << 31), "SEQ_EUNSUPPORTED"), (dict(len=1 << 31), "SEQ_EUNSUPPORTED"),
+    (dict(len=1 << 30, channels=1 << 12), "SEQ_EUNSUPPORTED"),
+    (dict(x=None), "SEQ_EINVAL"), (dict(r=None), "SEQ_EINVAL"), (dict(g=None), "SEQ_EINVAL"), (dict(rate=None), "SEQ_EINVAL"),
+    (dict(y=None), "SEQ_EINVAL"),
+    (dict(x=P + 1), "SEQ_EALIGN"), (dict(rate=P + 2), "SEQ_EALIGN"), (dict(state_out=P + 6 * GAP + 2), "SEQ_EALIGN"),
+    (dict(type=0, y=P + 5 * GAP + 2), "SEQ_EALIGN"), (dict(saved=P + 7 * GAP + 1), "SEQ_EALIGN"),
+    (dict(workspace=P + 8 * GAP + 8), "SEQ_EALIGN"),
+    (dict(y=P + 64), "SEQ_EINVAL"),                                  # y inside x
+    (dict(y=P, strides=[0, 64] + PLAIN[2:]), "SEQ_EINVAL"),          # y over an expanded x
+    (dict(strides=PLAIN[:6] + [ROW, 63]), "SEQ_EINVAL"),             # tokens of y overlap
+    (dict(strides=PLAIN[:6] + [64, 64]), "SEQ_EINVAL"),              # sequences of y overlap
+    (dict(strides=[-1, 64] + PLAIN[2:]), "SEQ_EINVAL"),
+    (dict(state_out=P + 4 * GAP + 4), "SEQ_EINVAL"),                 # state_out over a shifted state
+    (dict(saved=P + 6 * GAP + 4), "SEQ_EINVAL"),                     # saved over state_out
+    (dict(y=P + 2 * 191, strides=[100 * 192, 192] * 4), "SEQ_EINVAL"),  # a slice that reaches into the next one
+])
+def test_scan_refusals(L, change, code):
+    assert scan(L, **change) == getattr(L, code)
+
+
+BPLAIN = [ROW, 64] * 7
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(batch=-1), "SEQ_EINVAL"), (dict(type=9), "SEQ_EINVAL"), (dict(channels=0), "SEQ_EINVAL"),
+    (dict(batch=1 << 33), "SEQ_EUNSUPPORTED"),
+    (dict(dy=None), "SEQ_EINVAL"), (dict(saved=None), "SEQ_EINVAL"), (dict(dx=None), "SEQ_EINVAL"), (dict(drate=None), "SEQ_EINVAL"),
+    (dict(workspace=None), "SEQ_EINVAL"), (dict(workspace=P + 12 * GAP + 4), "SEQ_EALIGN"), (dict(dg=P + 9 * GAP + 1), "SEQ_EALIGN"),
+    (dict(drate=P + 10 * GAP + 1), "SEQ_EALIGN"),
+    (dict(dx=P + 2), "SEQ_EINVAL"),                                  # dx over a shifted dy
+    (dict(dx=P + 2 * GAP), "SEQ_EINVAL"),                            # dx over r
+    (dict(dr=P + 7 * GAP), "SEQ_EINVAL"),                            # dr over dx
+    (dict(strides=BPLAIN[:8] + [ROW, 1] + BPLAIN[10:]), "SEQ_EINVAL"),
+    (dict(dstate=P + 6 * GAP + 4), "SEQ_EINVAL"),
+    (dict(drate=P + 4 * GAP), "SEQ_EINVAL"),                         # drate over rate
+])
+def test_scan_gradient_refusals(L, change, code):
+    assert scan_back(L, **change) == getattr(L, code)
+
+
+def norm(L, **k):
+    a = dict(rows=10, channels=64, type=L.SEQ_FP16, x=P, y=P + GAP, z=P + 2 * GAP, strides=None, post=P + 3 * GAP, scale=P + 4 * GAP,
+             pre=P + 5 * GAP, eps=1e-5, out=P + 6 * GAP, normed=P + 7 * GAP, stats=P + 8 * GAP, stream=None)
+    a.update(k)
+    if a["strides"] is not None:
+        a["strides"] = L.int64s(a["strides"])
+    return L.lib.seq_norm_forward(*a.values())
+
+
+def norm_back(L, **k):
+    a = dict(rows=10, channels=64, type=L.SEQ_FP16, dout=P, dnormed=P + GAP, x=P + 2 * GAP, y=P + 3 * GAP, z=P + 4 * GAP, strides=None,
+             post=P + 5 * GAP, scale=P + 6 * GAP, pre=P + 7 * GAP, eps=1e-5, stats=P + 8 * GAP, dx=P + 9 * GAP, dy=P + 10 * GAP,
+             dz=P + 11 * GAP, dpost=P + 12 * GAP, dscale=P + 13 * GAP, dpre=P + 14 * GAP, workspace=P + 15 * GAP, stream=None)
+    a.update(k)
+    if a["strides"] is not None:
+        a["strides"] = L.int64s(a["strides"])
+    return L.lib.seq_norm_backward(*a.values())
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(rows=-1), "SEQ_EINVAL"), (dict(channels=0), "SEQ_EINVAL"), (dict(type=3), "SEQ_EINVAL"), (dict(eps=0.0), "SEQ_EINVAL"),
+    (dict(eps=float("nan")), "SEQ_EINVAL"), (dict(channels=65537), "SEQ_EUNSUPPORTED"), (dict(rows=1 << 31), "SEQ_EUNSUPPORTED"),
+    (dict(x=None), "SEQ_EINVAL"), (dict(y=None), "SEQ_EINVAL"), (dict(post=None), "SEQ_EINVAL"), (dict(out=None), "SEQ_EINVAL"),
+    (dict(pre=None), "SEQ_EINVAL"), (dict(normed=None), "SEQ_EINVAL"),
+    (dict(y=None, post=None, out=None), "SEQ_EINVAL"),               # a gate without a block
+    (dict(y=None, post=None, out=None, z=None, scale=None, pre=None, normed=None), "SEQ_EINVAL"),  # nothing to do
+    (dict(x=P + 1), "SEQ_EALIGN"), (dict(pre=P + 5 * GAP + 2), "SEQ_EALIGN"), (dict(stats=P + 8 * GAP + 2), "SEQ_EALIGN"),
+    (dict(out=P + 2), "SEQ_EINVAL"), (dict(out=P + GAP), "SEQ_EINVAL"), (dict(normed=P), "SEQ_EINVAL"),
+    (dict(normed=P + 6 * GAP), "SEQ_EINVAL"), (dict(strides=[64, 64, 64, 63, 64]), "SEQ_EINVAL"),
+    (dict(strides=[64, 64, 64, 64, -64]), "SEQ_EINVAL"), (dict(out=P, strides=[0, 64, 64, 64, 64]), "SEQ_EINVAL"),
+])
+def test_norm_refusals(L, change, code):
+    assert norm(L, **change) == getattr(L, code)
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(rows=-1), "SEQ_EINVAL"), (dict(type=7), "SEQ_EINVAL"), (dict(eps=-1.0), "SEQ_EINVAL"), (dict(channels=1 << 20), "SEQ_EUNSUPPORTED"),
+    (dict(x=None), "SEQ_EINVAL"), (dict(dx=None), "SEQ_EINVAL"), (dict(dy=None), "SEQ_EINVAL"), (dict(dz=None), "SEQ_EINVAL"),
+    (dict(stats=None), "SEQ_EINVAL"), (dict(workspace=None), "SEQ_EINVAL"), (dict(dnormed=None), "SEQ_EINVAL"), (dict(dpre=None), "SEQ_EINVAL"),
+    (dict(dscale=None), "SEQ_EINVAL"), (dict(scale=None), "SEQ_EINVAL"), (dict(dpost=None), "SEQ_EINVAL"),
+    (dict(workspace=P + 15 * GAP + 8), "SEQ_EALIGN"), (dict(dpre=P + 14 * GAP + 2), "SEQ_EALIGN"), (dict(dz=P + 11 * GAP + 1), "SEQ_EALIGN"),
+    (dict(dx=P + 2), "SEQ_EINVAL"), (dict(dx=P + GAP), "SEQ_EINVAL"), (dict(dy=P), "SEQ_EINVAL"), (dict(dz=P + 9 * GAP), "SEQ_EINVAL"),
+    (dict(strides=[64] * 7 + [1]), "SEQ_EINVAL"),
+])
+def test_norm_gradient_refusals(L, change, code):
+    assert norm_back(L, **change) == getattr(L, code)
+
+
+def test_nothing_to_do_is_no_error(L):
+    assert scan(L, batch=0, x=None, r=None, g=None, y=None) == L.SEQ_OK
+    assert norm(L, rows=0, x=None, y=None, z=None, out=None, normed=None, stats=None) == L.SEQ_OK
+
+
+def test_sizes(L):
+    assert L.lib.seq_scan_saved_bytes(3, 33, 7) == 3 * 3 * 7 * 4
+    assert L.lib.seq_scan_saved_bytes(3, 0, 7) == 0 and L.lib.seq_scan_saved_bytes(-1, 4, 7) == 0
+    for f in (0, 1):
+        assert L.lib.seq_scan_workspace_bytes(2, 100, 0, L.SEQ_FP32, f) == 0
+        assert L.lib.seq_scan_workspace_bytes(2, 100, 64, 5, f) == 0
+        assert L.lib.seq_scan_workspace_bytes(2, 100, 64, L.SEQ_FP32, f) % 16 == 0
+    assert L.lib.seq_norm_workspace_bytes(10, 0, 0) == 0 and L.lib.seq_norm_workspace_bytes(10, 64, 0) > 0
+
+
+def test_tensor_functions_refuse_what_they_cannot_take():
+    from paper_2609_32237_amd import seq_api as sq
+
+    x = torch.zeros(2, 3, 4)
+    with pytest.raises(TypeError):
+        sq.gated_scan(x, x, x, torch.zeros(4))  # not on a GPU
+    with pytest.raises(TypeError):
+        sq.residual_norm(torch.zeros(2, 3), pre=torch.ones(3), eps=1e-5)
+    with pytest.raises(TypeError):
+        sq.gated_scan(x.double(), x.double(), x.double(), torch.zeros(4))
+    with pytest.raises(ValueError):
+        sq.gated_scan_step(x, x, x, torch.zeros(4), torch.zeros(2, 4))
+
+
+def test_reference_gradients_against_differences():
+    """The 64-bit definitions that the kernels are compared with, by central differences in 64 bits."""
+    gen = torch.Generator().manual_seed(0)
+
+    def rand(*shape):
+        return torch.randn(*shape, generator=gen, dtype=torch.float64).requires_grad_(True)
+
+    n = torch.tensor([5, 0, 3], dtype=torch.int32)
+    assert torch.autograd.gradcheck(lambda *v: ref.scan(*v, n), (rand(3, 5, 2), rand(3, 5, 2), rand(3, 5, 2), rand(2), rand(3, 2)))
+    assert torch.autograd.gradcheck(lambda *v: ref.norm(*v, 1e-3), (rand(2, 5), rand(2, 5), rand(2, 5), rand(5), rand(5), rand(5)))
+
+
+def test_reference_matches_the_written_gradient():
+    """The closed form of the gradient that the header states, against the reference's."""
+    gen = torch.Generator().manual_seed(1)
+    x, r, g, dy = (torch.randn(2, 9, 3, generator=gen, dtype=torch.float64) for _ in range(4))
+    rate, state, dlast = torch.rand(3, dtype=torch.float64, generator=gen), torch.randn(2, 3, generator=gen, dtype=torch.float64), \
+        torch.randn(2, 3, generator=gen, dtype=torch.float64)
+    leaves = [v.clone().requires_grad_(True) for v in (x, r, g, rate, state)]
+    y, last = ref.scan(*leaves)
+    want = torch.autograd.grad((y, last), leaves, (dy, dlast))
+    sr, sg = ref.sigmoid(r), ref.sigmoid(g)
+    q, c, k, y = rate * sr, sg * x, dlast, y.detach()
+    dx, dr, dg, drate = torch.zeros_like(x), torch.zeros_like(x), torch.zeros_like(x), torch.zeros(3, dtype=torch.float64)
+    for t in range(8, -1, -1):
+        d = dy[:, t] + k
+        e = d * (c[:, t] - (y[:, t - 1] if t else state))
+        dx[:, t] = d * q[:, t] * sg[:, t]
+        dg[:, t] = dx[:, t] * x[:, t] * (1 - sg[:, t])
+        dr[:, t] = e * q[:, t] * (1 - sr[:, t])
+        drate += (e * sr[:, t]).sum(0)
+        k = (1 - q[:, t]) * d
+    for a, b in zip((dx, dr, dg, drate, k), want):
+        assert torch.allclose(a, b, rtol=1e-12, atol=1e-12)
