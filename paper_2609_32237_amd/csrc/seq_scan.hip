@@ -2,6 +2,8 @@
 // q = rate s(r), c = s(g) x, and its gradient.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "seq_device.hpp"
 #include "seq_host.hpp"
 
@@ -17,7 +19,11 @@ struct ScanArgs {
     int64_t xb, xt, rb, rt, gb, gt, yb, yt, dyb, dyt, dxb, dxt, drb, drt, dgb, dgt;
     const float *rate, *state, *dstate_out;
     const int32_t *lengths;
-    float *state_out, *saved, *dstate, *drate, *partial;
+    float *state_out, *saved, *dstate, *partial;
+    // how the call is cut: channel blocks, chains, tiles of a chain, chunks of 16 tokens
+    int64_t blocks, chains, tiles, chunks;
+    uint64_t *words;
+    unsigned *counter;
 };
 
 __device__ __forceinline__ int64_t valid_tokens(const ScanArgs &a, int64_t b) {
@@ -26,108 +32,485 @@ __device__ __forceinline__ int64_t valid_tokens(const ScanArgs &a, int64_t b) {
     return n < 0 ? 0 : n > a.len ? a.len : n;
 }
 
-// One thread per sequence and channel, token after token.
-template <typename E>
-__global__ void __launch_bounds__(256) scan_forward(ScanArgs a) {
-    using T = typename E::T;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.batch * a.channels) return;
-    const int64_t b = i / a.channels, d = i % a.channels, n = valid_tokens(a, b);
-    const int64_t chunks = (a.len + kChunk - 1) / kChunk;
-    const T *x = (const T *)a.x + b * a.xb + d, *r = (const T *)a.r + b * a.rb + d, *g = (const T *)a.g + b * a.gb + d;
-    T *y = (T *)a.y + b * a.yb + d;
-    const float rate = a.rate[d];
-    float h = a.state ? a.state[i] : 0.0f;
-    for (int64_t t = 0; t < a.len; ++t) {
-        if (a.saved && t % kChunk == 0) a.saved[(b * chunks + t / kChunk) * a.channels + d] = h;
-        float out = 0.0f;
-        if (t < n) {
-            const float q = rate * sigmoid(E::to_f(r[t * a.rt]));
-            const float c = sigmoid(E::to_f(g[t * a.gt])) * E::to_f(x[t * a.xt]);
-            h = fmaf(q, c - h, h);
-            out = h;
-        }
-        y[t * a.yt] = E::of_f(out);
-    }
-    if (a.state_out) a.state_out[i] = h;
+// The recurrence is a composition of maps h -> H + A h, one per token, with
+// A = 1 - q and H = q c, so it can be cut anywhere along the tokens.  A wave
+// takes 64 V channels of a chunk of 16 tokens, its lanes V adjacent channels
+// each; a workgroup takes W chunks that follow each other (a tile), and the
+// tiles of one sequence and channel block form a chain.  Each wave reads its
+// chunk once, keeps q and c in registers, and composes its 16 maps; the
+// composed maps pass through LDS, and with the state before its chunk each
+// wave runs the 16 steps again from registers and writes y.
+//
+// Between the tiles of a chain the state goes through one 64-bit word per
+// channel in the workspace: empty, the tile's composed map (A, H), or the
+// state behind the tile.  A tile first publishes its map, then composes the
+// maps of up to kWindow tiles before it onto the nearest state it finds, in
+// the order of the tokens: the tiles between do the same operations on the
+// same values, so the bits do not depend on how far it had to look.  The map
+// and what it is travel in one atomic word: no other memory has to be ordered.
+// Tiles are handed out by a counter, the earlier tiles of every chain first:
+// a tile waits only for tiles that started before it, and the first waits for
+// none, so every wait ends.
+constexpr int kWindow = 8;
+constexpr uint32_t kEmpty = 0xffffffffu, kState = 0xfffffffeu;  // in place of A: NaNs that no published A has
+// A word that never arrives (a workspace that another call writes) must not
+// hang the GPU: after this many polls, seconds, the state becomes NaN.
+constexpr int kMaxPolls = 1 << 22;
+
+__device__ __forceinline__ uint64_t map_word(float A, float H) {
+    const uint32_t a = A == A ? __float_as_uint(A) : 0x7fc00000u;
+    return (uint64_t)a << 32 | __float_as_uint(H);
+}
+__device__ __forceinline__ uint64_t state_word(float h) { return (uint64_t)kState << 32 | __float_as_uint(h); }
+__device__ __forceinline__ void publish(uint64_t *p, uint64_t w) {
+    __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t peek(const uint64_t *p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// One thread per sequence and channel, chunk after chunk from the last; the
-// states of a chunk are computed again from the saved one.
-template <typename E>
-__global__ void __launch_bounds__(256) scan_backward(ScanArgs a) {
-    using T = typename E::T;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.batch * a.channels) return;
-    const int64_t b = i / a.channels, d = i % a.channels, n = valid_tokens(a, b);
-    const int64_t chunks = (a.len + kChunk - 1) / kChunk;
-    const T *x = (const T *)a.x + b * a.xb + d, *r = (const T *)a.r + b * a.rb + d, *g = (const T *)a.g + b * a.gb + d;
-    const T *dy = (const T *)a.dy + b * a.dyb + d;
-    T *dx = (T *)a.dx + b * a.dxb + d, *dr = (T *)a.dr + b * a.drb + d, *dg = (T *)a.dg + b * a.dgb + d;
-    const float rate = a.rate[d];
-    float k = a.dstate_out ? a.dstate_out[i] : 0.0f, drate = 0.0f;
-    for (int64_t j = chunks - 1; j >= 0; --j) {
-        float h[kChunk + 1];
-        h[0] = a.saved[(b * chunks + j) * a.channels + d];
+// The state behind `before` tiles of a chain whose words start at `words`
+// (this lane's first channel; `pitch` words from tile to tile).
+template <int V>
+__device__ __forceinline__ void look_back(const uint64_t *words, int64_t pitch, int64_t before, float (&h)[V]) {
+    for (int poll = 0; poll < kMaxPolls; ++poll) {
+        const int window = poll == 0 ? 1 : kWindow;
+        uint64_t w[kWindow][V];
 #pragma unroll
-        for (int s = 0; s < kChunk; ++s) {
-            const int64_t t = j * kChunk + s;
-            h[s + 1] = h[s];
-            if (t < n) {
-                const float q = rate * sigmoid(E::to_f(r[t * a.rt]));
-                const float c = sigmoid(E::to_f(g[t * a.gt])) * E::to_f(x[t * a.xt]);
-                h[s + 1] = fmaf(q, c - h[s], h[s]);
-            }
-        }
+        for (int i = 0; i < kWindow; ++i)
+            if (i < window && i < before)
 #pragma unroll
-        for (int s = kChunk - 1; s >= 0; --s) {
-            const int64_t t = j * kChunk + s;
-            if (t < a.len) {
-                float ox = 0.0f, orr = 0.0f, og = 0.0f;
-                if (t < n) {
-                    const float sr = sigmoid(E::to_f(r[t * a.rt])), sg = sigmoid(E::to_f(g[t * a.gt]));
-                    const float xv = E::to_f(x[t * a.xt]), q = rate * sr;
-                    const float dh = E::to_f(dy[t * a.dyt]) + k;
-                    const float e = dh * (sg * xv - h[s]);
-                    drate = fmaf(e, sr, drate);
-                    orr = e * q * (1.0f - sr);
-                    ox = dh * q * sg;
-                    og = ox * xv * (1.0f - sg);
-                    k = fmaf(-q, dh, dh);
+                for (int j = 0; j < V; ++j) w[i][j] = peek(words + (before - 1 - i) * pitch + j);
+        bool have[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) have[j] = false;
+#pragma unroll
+        for (int i = kWindow - 1; i >= 0; --i)
+            if (i < window && i < before)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const uint32_t a = (uint32_t)(w[i][j] >> 32);
+                    const float v = __uint_as_float((uint32_t)w[i][j]);
+                    h[j] = a == kState ? v : fmaf(__uint_as_float(a), h[j], v);
+                    have[j] = a == kState || (have[j] && a != kEmpty);
                 }
-                dx[t * a.dxt] = E::of_f(ox);
-                dr[t * a.drt] = E::of_f(orr);
-                dg[t * a.dgt] = E::of_f(og);
+        bool all = true;
+#pragma unroll
+        for (int j = 0; j < V; ++j) all = all && have[j];
+        if (__all(all)) return;
+        if (poll) __builtin_amdgcn_s_sleep(1);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) h[j] = __builtin_nanf("");
+}
+
+// Sets the words of a chain to empty and the counter to 0.
+__global__ void __launch_bounds__(256) scan_clear(uint4 *words, int64_t quads, unsigned *counter) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < quads) words[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
+    if (i == 0) *counter = 0u;
+}
+
+// What a workgroup works on.
+template <int V, int W>
+struct Tile {
+    int64_t b, tile, col;  // sequence, place along the chain, first channel
+    int64_t chain;
+    int wave, lane, at;     // at: this lane's first channel from col on; lanes beyond the last one repeat it
+    bool live;
+    int64_t t0;             // first token of the wave's chunk
+    int count, write;       // its tokens that count, and that exist
+
+    template <bool BACK>
+    __device__ __forceinline__ void find(const ScanArgs &a, int64_t id) {
+        chain = id % a.chains, tile = id / a.chains;
+        if (BACK) tile = a.tiles - 1 - tile;
+        b = chain / a.blocks;
+        col = (chain % a.blocks) * (kWave * V);
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+        const int64_t last = a.channels - V - col;
+        live = lane * V <= last;
+        at = live ? lane * V : (int)last;
+        t0 = (tile * W + wave) * kChunk;
+        const int64_t n = valid_tokens(a, b) - t0, l = a.len - t0;
+        count = n < 0 ? 0 : n > kChunk ? kChunk : (int)n;
+        write = l < 0 ? 0 : l > kChunk ? kChunk : (int)l;
+    }
+};
+
+// The work of this workgroup: its index, or with chains the next of the counter.
+template <bool CHAIN>
+__device__ __forceinline__ int64_t next_tile(const ScanArgs &a) {
+    if (!CHAIN) return blockIdx.x;
+    __shared__ unsigned id;
+    if (threadIdx.x == 0) id = atomicAdd(a.counter, 1u);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(id);
+}
+
+template <typename E, int V, int W, bool CHAIN>
+__global__ void __launch_bounds__(kWave *W) scan_forward(ScanArgs a) {
+    using T = typename E::T;
+    __shared__ float2 maps[W][kWave * V];
+    __shared__ float carry[kWave * V];
+    Tile<V, W> k;
+    k.template find<false>(a, next_tile<CHAIN>(a));
+    const T *x = (const T *)a.x + k.b * a.xb + k.t0 * a.xt + k.col, *r = (const T *)a.r + k.b * a.rb + k.t0 * a.rt + k.col;
+    const T *g = (const T *)a.g + k.b * a.gb + k.t0 * a.gt + k.col;
+    const int64_t d = k.col + k.at;
+
+    float q[kChunk][V], c[kChunk][V], A[V], H[V], rate[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) A[j] = 1.0f, H[j] = 0.0f, rate[j] = a.rate[d + j];
+    auto gates = [&](auto full) {
+        Pack<E, V> px[kChunk], pr[kChunk], pg[kChunk];
+#pragma unroll
+        for (int s = 0; s < kChunk; ++s)
+            if (full || s < k.count) {
+                px[s].load(x + s * a.xt + k.at);
+                pr[s].load(r + s * a.rt + k.at);
+                pg[s].load(g + s * a.gt + k.at);
+            }
+#pragma unroll
+        for (int s = 0; s < kChunk; ++s)
+            if (full || s < k.count)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    q[s][j] = rate[j] * sigmoid(pr[s].get(j));
+                    c[s][j] = sigmoid(pg[s].get(j)) * px[s].get(j);
+                    H[j] = fmaf(q[s][j], c[s][j] - H[j], H[j]);
+                    A[j] = fmaf(-q[s][j], A[j], A[j]);
+                }
+    };
+    if (k.count == kChunk)
+        gates(std::true_type{});
+    else
+        gates(std::false_type{});
+    if (W > 1 || CHAIN) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) maps[k.wave][k.lane * V + j] = make_float2(A[j], H[j]);
+    }
+
+    float h[V];
+    if (W > 1 || CHAIN) __syncthreads();
+    if (k.wave == 0) {
+        float tA[V], tH[V];
+        uint64_t *words = a.words + k.chain * a.tiles * (kWave * V) + k.lane * V;
+        if (CHAIN && k.tile + 1 < a.tiles) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                tA[j] = A[j], tH[j] = H[j];
+                for (int w = 1; w < W; ++w) {
+                    const float2 m = maps[w][k.lane * V + j];
+                    tH[j] = fmaf(m.x, tH[j], m.y);
+                    tA[j] *= m.x;
+                }
+                if (k.tile > 0) publish(words + k.tile * (kWave * V) + j, map_word(tA[j], tH[j]));
+            }
+        }
+        if (!CHAIN || k.tile == 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) h[j] = a.state ? a.state[k.b * a.channels + d + j] : 0.0f;
+        } else {
+            look_back<V>(words, kWave * V, k.tile, h);
+        }
+        if (CHAIN && k.tile + 1 < a.tiles) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) publish(words + k.tile * (kWave * V) + j, state_word(fmaf(tA[j], h[j], tH[j])));
+        }
+        if (W > 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) carry[k.lane * V + j] = h[j];
+        }
+    }
+    if (W > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            h[j] = carry[k.lane * V + j];
+            for (int w = 0; w < k.wave; ++w) {
+                const float2 m = maps[w][k.lane * V + j];
+                h[j] = fmaf(m.x, h[j], m.y);
             }
         }
     }
-    if (a.dstate) a.dstate[i] = k;
-    a.partial[i] = drate;
+    if (a.saved && k.write && k.live) {
+        const int64_t chunk = k.t0 / kChunk;
+#pragma unroll
+        for (int j = 0; j < V; ++j) a.saved[(k.b * a.chunks + chunk) * a.channels + d + j] = h[j];
+    }
+    T *y = (T *)a.y + k.b * a.yb + k.t0 * a.yt + k.col;
+    auto states = [&](auto full) {
+#pragma unroll
+        for (int s = 0; s < kChunk; ++s)
+            if (full || s < k.write) {
+                float out[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    if (full || s < k.count) h[j] = fmaf(q[s][j], c[s][j] - h[j], h[j]);
+                    out[j] = full || s < k.count ? h[j] : 0.0f;
+                }
+                Pack<E, V> p;
+                p.set(out);
+                if (k.live) p.store(y + s * a.yt + k.at);
+            }
+    };
+    if (k.count == kChunk)
+        states(std::true_type{});
+    else
+        states(std::false_type{});
+    // the wave with the last token, or the first one where there is none
+    if (a.state_out && k.live && (k.write ? k.t0 + k.write == a.len : a.len == 0 && k.wave == 0)) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) a.state_out[k.b * a.channels + d + j] = h[j];
+    }
 }
 
-// drate of a channel: the partial sums in their order.
-__global__ void __launch_bounds__(256) scan_sum_rate(const float *partial, int64_t rows, int64_t channels, float *drate) {
-    const int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (d >= channels) return;
+// The gradient runs the same way from the last token to the first: the map of
+// a token is k -> (1 - q) (dy + k).  The states before each token are computed
+// again from the saved one of the chunk, in FP32: taken from y they would put
+// y's rounding into every term of drate.
+template <typename E, int V, int W, bool CHAIN>
+__global__ void __launch_bounds__(kWave *W) scan_backward(ScanArgs a) {
+    using T = typename E::T;
+    __shared__ float2 maps[W][kWave * V];
+    __shared__ float carry[kWave * V];
+    Tile<V, W> k;
+    k.template find<true>(a, next_tile<CHAIN>(a));
+    const T *x = (const T *)a.x + k.b * a.xb + k.t0 * a.xt + k.col, *r = (const T *)a.r + k.b * a.rb + k.t0 * a.rt + k.col;
+    const T *g = (const T *)a.g + k.b * a.gb + k.t0 * a.gt + k.col, *dy = (const T *)a.dy + k.b * a.dyb + k.t0 * a.dyt + k.col;
+    const int64_t d = k.col + k.at, chunk = k.t0 / kChunk;
+
+    // of each token: s(r), s(g), c - h before it, and x and dy as they are stored
+    float sr[kChunk][V], sg[kChunk][V], ch[kChunk][V], A[V], K[V], rate[V];
+    Pack<E, V> px[kChunk], pd[kChunk];
+#pragma unroll
+    for (int j = 0; j < V; ++j) A[j] = 1.0f, K[j] = 0.0f, rate[j] = a.rate[d + j];
+    auto gates = [&](auto full) {
+        Pack<E, V> pr[kChunk], pg[kChunk];
+        float h[V];
+#pragma unroll
+        for (int s = 0; s < kChunk; ++s)
+            if (full || s < k.count) {
+                pr[s].load(r + s * a.rt + k.at);
+                pg[s].load(g + s * a.gt + k.at);
+                px[s].load(x + s * a.xt + k.at);
+                pd[s].load(dy + s * a.dyt + k.at);
+            }
+        if (full || k.count) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) h[j] = a.saved[(k.b * a.chunks + chunk) * a.channels + d + j];
+        }
+#pragma unroll
+        for (int s = 0; s < kChunk; ++s)
+            if (full || s < k.count)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    sr[s][j] = sigmoid(pr[s].get(j));
+                    sg[s][j] = sigmoid(pg[s].get(j));
+                    ch[s][j] = sg[s][j] * px[s].get(j) - h[j];
+                    h[j] = fmaf(rate[j] * sr[s][j], ch[s][j], h[j]);
+                }
+#pragma unroll
+        for (int s = kChunk - 1; s >= 0; --s)
+            if (full || s < k.count)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float q = rate[j] * sr[s][j], dh = pd[s].get(j) + K[j];
+                    K[j] = fmaf(-q, dh, dh);
+                    A[j] = fmaf(-q, A[j], A[j]);
+                }
+    };
+    if (k.count == kChunk)
+        gates(std::true_type{});
+    else
+        gates(std::false_type{});
+    if (W > 1 || CHAIN) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) maps[k.wave][k.lane * V + j] = make_float2(A[j], K[j]);
+    }
+
+    float kk[V];
+    if (W > 1 || CHAIN) __syncthreads();
+    if (k.wave == W - 1) {
+        float tA[V], tK[V];
+        uint64_t *words = a.words + k.chain * a.tiles * (kWave * V) + k.lane * V;
+        const int64_t place = a.tiles - 1 - k.tile;  // along the chain
+        if (CHAIN && k.tile > 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                tA[j] = A[j], tK[j] = K[j];
+                for (int w = W - 2; w >= 0; --w) {
+                    const float2 m = maps[w][k.lane * V + j];
+                    tK[j] = fmaf(m.x, tK[j], m.y);
+                    tA[j] *= m.x;
+                }
+                if (place > 0) publish(words + place * (kWave * V) + j, map_word(tA[j], tK[j]));
+            }
+        }
+        if (!CHAIN || place == 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) kk[j] = a.dstate_out ? a.dstate_out[k.b * a.channels + d + j] : 0.0f;
+        } else {
+            look_back<V>(words, kWave * V, place, kk);
+        }
+        if (CHAIN && k.tile > 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) publish(words + place * (kWave * V) + j, state_word(fmaf(tA[j], kk[j], tK[j])));
+        }
+        if (W > 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) carry[k.lane * V + j] = kk[j];
+        }
+    }
+    if (W > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            kk[j] = carry[k.lane * V + j];
+            for (int w = W - 1; w > k.wave; --w) {
+                const float2 m = maps[w][k.lane * V + j];
+                kk[j] = fmaf(m.x, kk[j], m.y);
+            }
+        }
+    }
+    T *dx = (T *)a.dx + k.b * a.dxb + k.t0 * a.dxt + k.col, *dr = (T *)a.dr + k.b * a.drb + k.t0 * a.drt + k.col;
+    T *dg = (T *)a.dg + k.b * a.dgb + k.t0 * a.dgt + k.col;
+    float drate[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) drate[j] = 0.0f;
+    auto gradients = [&](auto full) {
+#pragma unroll
+        for (int s = kChunk - 1; s >= 0; --s)
+            if (full || s < k.write) {
+                float ox[V], orr[V], og[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    ox[j] = orr[j] = og[j] = 0.0f;
+                    if (full || s < k.count) {
+                        const float q = rate[j] * sr[s][j], dh = pd[s].get(j) + kk[j], e = dh * ch[s][j];
+                        drate[j] = fmaf(e, sr[s][j], drate[j]);
+                        orr[j] = e * q * (1.0f - sr[s][j]);
+                        ox[j] = dh * q * sg[s][j];
+                        og[j] = ox[j] * px[s].get(j) * (1.0f - sg[s][j]);
+                        kk[j] = fmaf(-q, dh, dh);
+                    }
+                }
+                Pack<E, V> ax, ar, ag;
+                ax.set(ox), ar.set(orr), ag.set(og);
+                if (k.live) {
+                    ax.store(dx + s * a.dxt + k.at);
+                    ar.store(dr + s * a.drt + k.at);
+                    ag.store(dg + s * a.dgt + k.at);
+                }
+            }
+    };
+    if (k.count == kChunk)
+        gradients(std::true_type{});
+    else
+        gradients(std::false_type{});
+    if (a.dstate && k.live && k.tile == 0 && k.wave == 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) a.dstate[k.b * a.channels + d + j] = kk[j];
+    }
+    // the tile's part of drate: its waves' in their order
+    if (W > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < V; ++j) maps[k.wave][k.lane * V + j].x = drate[j];
+        __syncthreads();
+        if (k.wave == 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                for (int w = 1; w < W; ++w) drate[j] += maps[w][k.lane * V + j].x;
+        }
+    }
+    if (k.wave == 0 && k.live) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) a.partial[(k.tile * a.batch + k.b) * a.channels + d + j] = drate[j];
+    }
+}
+
+// drate of a channel from the tiles' parts: 16 groups of rows, joined in order.
+constexpr int kSumGroups = 16;
+__global__ void __launch_bounds__(kWave *kSumGroups) scan_sum_rate(const float *partial, int64_t rows, int64_t channels, float *drate) {
+    __shared__ float part[kSumGroups][kWave];
+    const int lane = threadIdx.x % kWave, group = threadIdx.x / kWave;
+    const int64_t d = (int64_t)blockIdx.x * kWave + lane;
     float s = 0.0f;
-    for (int64_t k = 0; k < rows; ++k) s += partial[k * channels + d];
-    drate[d] = s;
+    if (d < channels)
+        for (int64_t k = group; k < rows; k += kSumGroups) s += partial[k * channels + d];
+    part[group][lane] = s;
+    __syncthreads();
+    if (group == 0 && d < channels) {
+        for (int k = 1; k < kSumGroups; ++k) s += part[k][lane];
+        drate[d] = s;
+    }
+}
+
+// How a call is cut: channels per lane, waves per workgroup, tiles per chain.
+struct Cut {
+    int lane, waves;
+    int64_t blocks, chains, tiles, groups;
+    size_t words_bytes() const { return tiles > 1 ? (size_t)(chains * tiles) * (size_t)(kWave * lane) * sizeof(uint64_t) : 0; }
+};
+
+Cut cut_of(int64_t batch, int64_t len, int64_t channels, int type) {
+    Cut c;
+    // Two adjacent 16-bit channels per lane make 256-byte rows of a wave, as one
+    // FP32 channel does; an odd number of channels is taken one by one.
+    c.lane = type != SEQ_FP32 && channels % 2 == 0 ? 2 : 1;
+    const int64_t chunks = ceil_div(len, kChunk);
+    c.waves = chunks <= 1 ? 1 : chunks <= 2 ? 2 : chunks <= 4 ? 4 : 8;
+    c.tiles = chunks ? ceil_div(chunks, c.waves) : 1;
+    c.blocks = ceil_div(channels, kWave * c.lane);
+    c.chains = batch * c.blocks;
+    c.groups = c.chains * c.tiles;
+    return c;
+}
+
+template <bool BACK, typename E, int V, int W>
+const void *kernel_of(bool chain) {
+    if (BACK) return chain ? (const void *)scan_backward<E, V, W, W == 8> : (const void *)scan_backward<E, V, W, false>;
+    return chain ? (const void *)scan_forward<E, V, W, W == 8> : (const void *)scan_forward<E, V, W, false>;
+}
+template <bool BACK, typename E, int V>
+const void *kernel_of(const Cut &c) {
+    const bool chain = c.tiles > 1;
+    return c.waves == 1 ? kernel_of<BACK, E, V, 1>(chain)
+                        : c.waves == 2 ? kernel_of<BACK, E, V, 2>(chain)
+                                       : c.waves == 4 ? kernel_of<BACK, E, V, 4>(chain) : kernel_of<BACK, E, V, 8>(chain);
+}
+template <bool BACK>
+const void *kernel_of(const Cut &c, int type) {
+    if (type == SEQ_FP32) return kernel_of<BACK, F32, 1>(c);
+    if (type == SEQ_FP16) return c.lane == 2 ? kernel_of<BACK, F16, 2>(c) : kernel_of<BACK, F16, 1>(c);
+    return c.lane == 2 ? kernel_of<BACK, BF16, 2>(c) : kernel_of<BACK, BF16, 1>(c);
+}
+
+// The workspace: the chains' words, the counter, and for the gradient the tiles' parts of drate.
+constexpr size_t kCounterBytes = 16;
+size_t counter_offset(const Cut &c) { return c.words_bytes(); }
+size_t partial_offset(const Cut &c) { return c.tiles > 1 ? c.words_bytes() + kCounterBytes : 0; }
+size_t partial_bytes(const Cut &c, int64_t batch, int64_t channels) { return up16((size_t)(c.tiles * batch * channels) * sizeof(float)); }
+
+// Fills in the cut and the workspace, and clears what the chains start from.
+int start(ScanArgs &a, const Cut &c, void *workspace, hipStream_t stream) {
+    a.blocks = c.blocks, a.chains = c.chains, a.tiles = c.tiles, a.chunks = ceil_div(a.len, kChunk);
+    if (c.tiles <= 1) return SEQ_OK;
+    a.words = (uint64_t *)workspace;
+    a.counter = (unsigned *)((char *)workspace + counter_offset(c));
+    void *words = workspace;
+    int64_t quads = (int64_t)(c.words_bytes() / 16);
+    void *args[] = {&words, &quads, &a.counter};
+    return launch((const void *)scan_clear, dim3((unsigned)ceil_div(quads, 256)), dim3(256), args, 0, stream);
 }
 
 bool sizes_ok(int64_t batch, int64_t len, int64_t channels) { return batch >= 0 && len >= 0 && channels >= 1; }
 bool sizes_supported(int64_t batch, int64_t len, int64_t channels) {
     if (batch > kMaxSize || len > kMaxSize || channels > kMaxSize) return false;
     const __int128 n = (__int128)batch * (len > 0 ? len : 1) * channels;
-    return n <= kMaxElements && ceil_div(batch * channels, 256) <= kMaxSize;
-}
-
-const void *forward_kernel(int type) {
-    return type == SEQ_FP32 ? (const void *)scan_forward<F32>
-                            : type == SEQ_FP16 ? (const void *)scan_forward<F16> : (const void *)scan_forward<BF16>;
-}
-const void *backward_kernel(int type) {
-    return type == SEQ_FP32 ? (const void *)scan_backward<F32>
-                            : type == SEQ_FP16 ? (const void *)scan_backward<F16> : (const void *)scan_backward<BF16>;
+    return n <= kMaxElements && cut_of(batch, len, channels, SEQ_FP32).groups <= kMaxSize;
 }
 
 }  // namespace
@@ -144,7 +527,8 @@ size_t seq_scan_saved_bytes(int64_t batch, int64_t len, int64_t channels) {
 
 size_t seq_scan_workspace_bytes(int64_t batch, int64_t len, int64_t channels, int type, int backward) {
     if (!sizes_ok(batch, len, channels) || !sizes_supported(batch, len, channels) || !known_type(type)) return 0;
-    return backward ? up16((size_t)(batch * channels) * sizeof(float)) : 0;
+    const Cut c = cut_of(batch, len, channels, type);
+    return partial_offset(c) + (backward ? partial_bytes(c, batch, channels) : 0);
 }
 
 int seq_scan_forward(int64_t batch, int64_t len, int64_t channels, int type, const void *x, const void *r,
@@ -190,8 +574,11 @@ int seq_scan_forward(int64_t batch, int64_t len, int64_t channels, int type, con
     a.xb = in[0].so, a.xt = in[0].si, a.rb = in[1].so, a.rt = in[1].si, a.gb = in[2].so, a.gt = in[2].si;
     a.yb = out.so, a.yt = out.si;
     a.rate = rate, a.state = state, a.lengths = lengths, a.state_out = state_out, a.saved = saved;
+    const Cut c = cut_of(batch, len, channels, type);
+    const int rc = start(a, c, workspace, stream);
+    if (rc != SEQ_OK) return rc;
     void *args[] = {&a};
-    return launch(forward_kernel(type), dim3((unsigned)ceil_div(states, 256)), dim3(256), args, 0, stream);
+    return launch(kernel_of<false>(c, type), dim3((unsigned)c.groups), dim3(kWave * c.waves), args, 0, stream);
 }
 
 int seq_scan_backward(int64_t batch, int64_t len, int64_t channels, int type, const void *dy, const void *x,
@@ -237,15 +624,20 @@ int seq_scan_backward(int64_t batch, int64_t len, int64_t channels, int type, co
     a.gb = v[3].so, a.gt = v[3].si, a.dxb = v[4].so, a.dxt = v[4].si, a.drb = v[5].so, a.drt = v[5].si;
     a.dgb = v[6].so, a.dgt = v[6].si;
     a.rate = rate, a.saved = const_cast<float *>(saved), a.lengths = lengths, a.dstate_out = dstate_out;
-    a.drate = drate, a.dstate = dstate, a.partial = (float *)workspace;
+    a.dstate = dstate;
+    const Cut c = cut_of(batch, len, channels, type);
+    a.partial = (float *)((char *)workspace + partial_offset(c));
     if (states) {
+        int rc = start(a, c, workspace, stream);
+        if (rc != SEQ_OK) return rc;
         void *args[] = {&a};
-        const int rc = launch(backward_kernel(type), dim3((unsigned)ceil_div(states, 256)), dim3(256), args, 0, stream);
+        rc = launch(kernel_of<true>(c, type), dim3((unsigned)c.groups), dim3(kWave * c.waves), args, 0, stream);
         if (rc != SEQ_OK) return rc;
     }
     const float *partial = a.partial;
-    void *args[] = {&partial, &batch, &channels, &drate};
-    return launch((const void *)scan_sum_rate, dim3((unsigned)ceil_div(channels, 256)), dim3(256), args, 0, stream);
+    int64_t rows = batch * c.tiles;
+    void *args[] = {&partial, &rows, &channels, &drate};
+    return launch((const void *)scan_sum_rate, dim3((unsigned)ceil_div(channels, kWave)), dim3(kWave * kSumGroups), args, 0, stream);
 }
 
 const char *seq_strerror(int code) {
