@@ -5,13 +5,15 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 namespace mi355seq {
 
 constexpr int kWave = 64;
 
 // Element types.  to_f is exact; of_f is the one rounding of an activation
-// (to nearest, ties to even), done where it is written.
+// (to nearest, ties to even), done where it is written.  The 16-bit types are
+// taken from and put into words of two, so that a row stays packed in registers.
 struct F32 {
     using T = float;
     static __device__ __forceinline__ float to_f(T v) { return v; }
@@ -19,19 +21,55 @@ struct F32 {
 };
 struct F16 {
     using T = _Float16;
+    using T2 = T __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ float to_f(T v) { return (float)v; }
     static __device__ __forceinline__ T of_f(float v) { return (T)v; }
+    static __device__ __forceinline__ float half_of(uint32_t w, int high) {
+        T2 v;
+        __builtin_memcpy(&v, &w, 4);
+        return (float)(high ? v.y : v.x);
+    }
+    static __device__ __forceinline__ uint32_t two(float low, float high) {
+        const T2 v{(T)low, (T)high};
+        uint32_t w;
+        __builtin_memcpy(&w, &v, 4);
+        return w;
+    }
 };
 struct BF16 {
     using T = __bf16;
+    using T2 = T __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ float to_f(T v) { return (float)v; }
     static __device__ __forceinline__ T of_f(float v) { return (T)v; }
+    static __device__ __forceinline__ float half_of(uint32_t w, int high) {
+        return __uint_as_float(high ? w & 0xffff0000u : w << 16);
+    }
+    static __device__ __forceinline__ uint32_t two(float low, float high) {
+        const T2 v{(T)low, (T)high};
+        uint32_t w;
+        __builtin_memcpy(&w, &v, 4);
+        return w;
+    }
 };
 
 // 1 / (1 + e^-v) with the hardware's exp2 and reciprocal (each within 1 ulp):
 // 0 at -inf, 1 at +inf, relative error about |v| 2^-24 + 3e-7.
 __device__ __forceinline__ float sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * v));
+}
+
+// Sum over the wave, the same in every lane: 4 steps of cross-lane moves make
+// the sums of 16 lanes, four of those are read to scalar registers.
+__device__ __forceinline__ float wave_sum(float v) {
+    auto moved = [](float x, auto ctrl) {
+        return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    v += moved(v, std::integral_constant<int, 0xb1>{});   // lanes 1 0 3 2 of each four
+    v += moved(v, std::integral_constant<int, 0x4e>{});   // lanes 2 3 0 1
+    v += moved(v, std::integral_constant<int, 0x124>{});  // rotated by 4 within 16
+    v += moved(v, std::integral_constant<int, 0x128>{});  // rotated by 8
+    auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+    return (lane(0) + lane(16)) + (lane(32) + lane(48));
 }
 
 // V consecutive elements in one access of up to 16 bytes.  Accesses need no
@@ -58,16 +96,66 @@ struct Pack {
 
     __device__ __forceinline__ void load(const T *p) { u = ((const Unaligned *)p)->u; }
     __device__ __forceinline__ void store(T *p) const { ((Unaligned *)p)->u = u; }
-    __device__ __forceinline__ float get(int j) const {
-        T v[V];
-        __builtin_memcpy(v, &u, sizeof(u));
-        return E::to_f(v[j]);
-    }
-    __device__ __forceinline__ void set(const float (&f)[V]) {
-        T v[V];
+    // Keeps the stored form: what was converted from it before is converted
+    // again after this, instead of being held in twice the registers.
+    __device__ __forceinline__ void hold() { asm volatile("" : "+v"(u)); }
+    // elements `at` .. of a row of `end`, zeros behind it
+    __device__ __forceinline__ void load(const T *row, int at, int end) {
+        if (at + V <= end) {
+            load(row + at);
+        } else {
+            T v[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = E::of_f(f[j]);
-        __builtin_memcpy(&u, v, sizeof(u));
+            for (int j = 0; j < V; ++j) v[j] = at + j < end ? row[at + j] : (T)0.0f;
+            __builtin_memcpy(&u, v, sizeof(u));
+        }
+    }
+    __device__ __forceinline__ void store(T *row, int at, int end) const {
+        if (at + V <= end) {
+            store(row + at);
+        } else {
+            T v[V];
+            __builtin_memcpy(v, &u, sizeof(u));
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (at + j < end) row[at + j] = v[j];
+        }
+    }
+    // the word that holds element j of a 16-bit pack
+    __device__ __forceinline__ uint32_t word(int j) const {
+        if constexpr (V * sizeof(T) <= 4)
+            return u;
+        else
+            return u[j / 2];
+    }
+    __device__ __forceinline__ float get(int j) const {
+        if constexpr (sizeof(T) == 2 && V > 1) {
+            return E::half_of(word(j), j % 2);
+        } else {
+            T v[V];
+            __builtin_memcpy(v, &u, sizeof(u));
+            return E::to_f(v[j]);
+        }
+    }
+    // elements COUNT i .. COUNT i + COUNT - 1
+    template <int COUNT>
+    __device__ __forceinline__ void set(int i, const float (&f)[COUNT]) {
+        if constexpr (sizeof(T) == 2 && V > 1) {
+#pragma unroll
+            for (int k = 0; k < COUNT / 2; ++k) {
+                const uint32_t w = E::two(f[2 * k], f[2 * k + 1]);
+                if constexpr (V * sizeof(T) <= 4)
+                    u = w;
+                else
+                    u[COUNT / 2 * i + k] = w;
+            }
+        } else {
+            T v[V];
+            __builtin_memcpy(v, &u, sizeof(u));
+#pragma unroll
+            for (int j = 0; j < COUNT; ++j) v[COUNT * i + j] = E::of_f(f[j]);
+            __builtin_memcpy(&u, v, sizeof(u));
+        }
     }
 };
 

@@ -8,9 +8,8 @@
 namespace mi355seq {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int64_t kMaxChannels = 65536;
-constexpr int kRowGroups = 64;  // partial sums of each column
+constexpr int kMaxHeld = 16384;  // widest row that a workgroup holds in registers
 
 struct NormArgs {
     int64_t rows;
@@ -20,79 +19,360 @@ struct NormArgs {
     void *out, *normed, *dx, *dy, *dz;
     int64_t xs, ys, zs, outs, normeds, douts, dnormeds, dxs, dys, dzs;
     const float *post, *scale, *pre;
-    float *stats, *mean, *partial, *dpost, *dscale, *dpre;
+    float *stats, *partial, *dpost, *dscale, *dpre;
 };
-
-__device__ __forceinline__ float block_sum(float v) {
-    __shared__ float part[kThreads / kWave];
-#pragma unroll
-    for (int m = kWave / 2; m > 0; m /= 2) v += __shfl_xor(v, m);
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
-    __syncthreads();
-    float s = 0.0f;
-    for (int w = 0; w < kThreads / kWave; ++w) s += part[w];
-    return s;
-}
-
-// scale * post of one channel
-__device__ __forceinline__ float weight(const NormArgs &a, int d) { return a.post[d] * (a.scale ? a.scale[d] : 1.0f); }
 
 // v - vh mean(v vh) of a row vh of norm 1 - eps i^2: with one channel it is
 // v eps i^2, of which the difference of two FP32 values would leave nothing.
 // So there the factor is that and the mean is 0.
 __device__ __forceinline__ float one_channel(const NormArgs &a, float i) { return a.channels == 1 ? a.eps * i * i : 1.0f; }
 
+// Sums over the workgroup's threads, `count` of them at once; one barrier.  Two
+// buffers in turn: who writes a buffer again has passed the other's barrier,
+// which every reader of the first use reached after reading.
+template <int THREADS, int COUNT>
+struct GroupSum {
+    static constexpr int kWaves = THREADS / kWave;
+    float (*buffers)[COUNT][kWaves];
+    int turn = 0;
+
+    __device__ __forceinline__ void operator()(float (&v)[COUNT]) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = wave_sum(v[i]);
+        if (kWaves == 1) return;
+        auto &part = buffers[turn];
+        if (threadIdx.x % kWave == 0) {
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) part[i][threadIdx.x / kWave] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            v[i] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v[i] += part[i][w];
+        }
+        turn ^= 1;
+    }
+};
+
+// A row is held in registers by THREADS lanes, N accesses of 16 bytes each: a
+// wave for short rows (four rows to a workgroup, no barrier), else a workgroup.
+// The rows go round the grid, so that the weights (FP32: as many bytes as the
+// activations or more) are read once by a workgroup and kept in LDS, laid out
+// so that each lane reads four of its own at once and a wave all banks.
+template <int THREADS>
+constexpr int kRowsAtOnce = THREADS == kWave ? 4 : 1;
+
+template <typename E, int N, int THREADS>
+struct Held {
+    using T = typename E::T;
+    static constexpr int V = 16 / sizeof(T);
+    static constexpr int kWeights = N * THREADS * V;  // floats of LDS for one row of weights
+    using P = Pack<E, V>;
+    int lane, end;
+
+    __device__ __forceinline__ explicit Held(int channels) : lane(threadIdx.x % THREADS), end(channels) {}
+    // first channel of access n
+    __device__ __forceinline__ int at(int n) const { return (n * THREADS + lane) * V; }
+    // a row of an activation; zeros where there is none
+    __device__ __forceinline__ void load(P (&p)[N], const void *base, int64_t row, int64_t stride) const {
+        const T *r = (const T *)base + row * stride;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            p[n].u = typename P::U{};
+            if (base) p[n].load(r, at(n), end);
+        }
+    }
+    __device__ __forceinline__ void store(const P &p, int n, void *base, int64_t row, int64_t stride) const {
+        p.store((T *)base + row * stride, at(n), end);
+    }
+    // a row of weights (times another one) into LDS; zeros where there is none
+    __device__ __forceinline__ void keep(float *lds, const float *of, const float *times) const {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int d = at(n) + j;
+                float w = 0.0f;
+                if (of && d < end) w = times ? of[d] * times[d] : of[d];
+                lds[((n * (V / 4) + j / 4) * THREADS + lane) * 4 + j % 4] = w;
+            }
+    }
+    // four weights of access n, from 4 q on
+    __device__ __forceinline__ void weights(float (&w)[4], const float *lds, int n, int q) const {
+        const float4 f = *(const float4 *)(lds + ((n * (V / 4) + q) * THREADS + lane) * 4);
+        w[0] = f.x, w[1] = f.y, w[2] = f.z, w[3] = f.w;
+    }
+};
+
+template <typename E, int N, int THREADS>
+__global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_forward(NormArgs a) {
+    using R = Held<E, N, THREADS>;
+    constexpr int V = R::V;
+    extern __shared__ float4 lds[];
+    __shared__ float buffers[2][1][THREADS / kWave];
+    float *lw = (float *)lds, *lpre = lw + R::kWeights;
+    GroupSum<THREADS, 1> sum{buffers};
+    const R at(a.channels);
+    if (threadIdx.x < THREADS) {
+        at.keep(lw, a.post, a.scale);
+        at.keep(lpre, a.pre, nullptr);
+    }
+    __syncthreads();
+    const bool has_z = a.z != nullptr;
+    const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<THREADS>;
+    int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<THREADS>;
+    if (THREADS == kWave) row += __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    for (; row < a.rows; row += step) {
+        typename R::P px[N], py[N], pz[N];
+        at.load(py, a.y, row, a.ys);
+        at.load(px, a.x, row, a.xs);
+        at.load(pz, a.z, row, a.zs);
+        float o[N][V], iy = 0.0f, io = 0.0f;
+        if (a.y) {
+            float s[1] = {0.0f};
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) s[0] = fmaf(py[n].get(j), py[n].get(j), s[0]);
+                py[n].hold();
+            }
+            sum(s);
+            iy = 1.0f / sqrtf(fmaf(s[0], a.inv_channels, a.eps));
+        }
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            typename R::P p;
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) {
+                float w[4], f[4];
+                at.weights(w, lw, n, i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int j = 4 * i + k;
+                    const float gate = has_z ? pz[n].get(j) * sigmoid(pz[n].get(j)) : 1.0f;
+                    f[k] = fmaf(w[k] * gate, py[n].get(j) * iy, px[n].get(j));
+                    s[0] = fmaf(f[k], f[k], s[0]);
+                    o[n][j] = f[k];
+                }
+                p.set(i, f);
+            }
+            if (a.out) at.store(p, n, a.out, row, a.outs);
+        }
+        if (a.pre) {
+            sum(s);
+            io = 1.0f / sqrtf(fmaf(s[0], a.inv_channels, a.eps));
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                typename R::P p;
+#pragma unroll
+                for (int i = 0; i < V / 4; ++i) {
+                    float pre[4];
+                    at.weights(pre, lpre, n, i);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) pre[k] *= o[n][4 * i + k] * io;
+                    p.set(i, pre);
+                }
+                at.store(p, n, a.normed, row, a.normeds);
+            }
+        }
+        if (a.stats && at.lane < 2) a.stats[2 * row + at.lane] = at.lane ? io : iy;
+    }
+}
+
+// One reduction a row.  With oh = o / rms(o), p = weight G m and v = dnormed pre,
+// t = dout + (v - oh mean(v oh)) / rms(o), so the second mean, of t p, is a
+// combination of sums that need no t:
+//     mean(t p) = mean((dout + v / rms(o)) p) - mean(v oh) / rms(o) mean(oh p).
+// The sums for the weights' gradients stay in each lane's registers over its
+// rows; every workgroup writes its own, and norm_sum joins them in order.
+template <typename E, int N, int THREADS>
+__global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(NormArgs a) {
+    using R = Held<E, N, THREADS>;
+    constexpr int V = R::V;
+    extern __shared__ float4 lds[];
+    __shared__ float buffers[2][3][THREADS / kWave];
+    float *lw = (float *)lds, *lpre = lw + R::kWeights;
+    GroupSum<THREADS, 3> sum{buffers};
+    const R at(a.channels);
+    if (threadIdx.x < THREADS) {
+        at.keep(lw, a.post, a.scale);
+        at.keep(lpre, a.pre, nullptr);
+    }
+    __syncthreads();
+    const bool has_z = a.z != nullptr, has_pre = a.pre != nullptr;
+    float dw[N][V], dpre[N][V];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int j = 0; j < V; ++j) dw[n][j] = dpre[n][j] = 0.0f;
+    const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<THREADS>;
+    int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<THREADS>;
+    if (THREADS == kWave) row += __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    for (; row < a.rows; row += step) {
+        typename R::P px[N], py[N], pz[N], po[N], pn[N];
+        const float iy = a.stats[2 * row], io = a.stats[2 * row + 1];
+        at.load(px, a.x, row, a.xs);
+        at.load(py, a.y, row, a.ys);
+        at.load(pz, a.z, row, a.zs);
+        at.load(pn, a.dnormed, row, a.dnormeds);
+        at.load(po, a.dout, row, a.douts);
+        float sg[N][V], s[3] = {0.0f, 0.0f, 0.0f};
+        // of one element: o, the gate, m
+        auto forward = [&](int n, int j, float w, float &gate, float &m) {
+            m = py[n].get(j) * iy;
+            gate = has_z ? pz[n].get(j) * sg[n][j] : 1.0f;
+            const float o = fmaf(w * gate, m, px[n].get(j));
+            return o;
+        };
+        // Four channels at a time, in this order: taken all at once, the
+        // conversions alone would fill the registers.
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) {
+                float w[4], pre[4];
+                at.weights(w, lw, n, i);
+                at.weights(pre, lpre, n, i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int j = 4 * i + k;
+                    sg[n][j] = sigmoid(pz[n].get(j));
+                    float gate, m;
+                    const float oh = forward(n, j, w[k], gate, m) * io, p = w[k] * gate * m, v = pn[n].get(j) * pre[k];
+                    s[0] = fmaf(v, oh, s[0]);
+                    s[1] = fmaf(fmaf(io, v, po[n].get(j)), p, s[1]);
+                    s[2] = fmaf(oh, p, s[2]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            px[n].hold(), py[n].hold(), pz[n].hold(), pn[n].hold(), po[n].hold();
+        }
+        sum(s);
+        const bool one = a.channels == 1;
+        const float mean = one || !has_pre ? 0.0f : io * s[0] * a.inv_channels;
+        const float mean_y = one ? 0.0f : (has_pre ? s[1] - mean * s[2] : s[1]) * a.inv_channels;
+        const float fo = io * one_channel(a, io), fy = one_channel(a, iy);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            typename R::P gx, gy, gz;
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) {
+                float w[4], pre[4], dx[4], dy[4], dz[4];
+                at.weights(w, lw, n, i);
+                at.weights(pre, lpre, n, i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int j = 4 * i + k;
+                    float gate, m;
+                    const float oh = forward(n, j, w[k], gate, m) * io, dn = pn[n].get(j);
+                    dpre[n][j] = fmaf(dn, oh, dpre[n][j]);
+                    const float t = po[n].get(j) + (has_pre ? fo * (dn * pre[k]) - mean * oh : 0.0f), tw = t * w[k];
+                    dw[n][j] = fmaf(t * gate, m, dw[n][j]);
+                    dx[k] = t;
+                    dy[k] = iy * (tw * gate * fy - m * mean_y);
+                    dz[k] = tw * m * fmaf(gate, 1.0f - sg[n][j], sg[n][j]);
+                }
+                gx.set(i, dx);
+                gy.set(i, dy);
+                gz.set(i, dz);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            at.store(gx, n, a.dx, row, a.dxs);
+            if (a.y) at.store(gy, n, a.dy, row, a.dys);
+            if (a.z) at.store(gz, n, a.dz, row, a.dzs);
+        }
+    }
+    // this workgroup's (for short rows: this wave's) part of the weights' gradients
+    int64_t slot = blockIdx.x;
+    if (THREADS == kWave) slot = slot * kRowsAtOnce<THREADS> + threadIdx.x / kWave;
+    float *part = a.partial + 2 * slot * a.channels;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (at.at(n) + j < a.channels) {
+                part[at.at(n) + j] = dw[n][j];
+                part[a.channels + at.at(n) + j] = dpre[n][j];
+            }
+}
+
+// The weights' gradients from the parts: 32 channels to a workgroup, 32 groups
+// of parts joined in order.
+constexpr int kSumChannels = 32, kSumGroups = 32;
+__global__ void __launch_bounds__(kSumChannels *kSumGroups) norm_sum(NormArgs a, int parts) {
+    __shared__ float sums[2][kSumGroups][kSumChannels];
+    const int c = threadIdx.x % kSumChannels, group = threadIdx.x / kSumChannels, d = blockIdx.x * kSumChannels + c;
+    float p = 0.0f, dpre = 0.0f;
+    if (d < a.channels)
+        for (int k = group; k < parts; k += kSumGroups) {
+            p += a.partial[2 * (int64_t)k * a.channels + d];
+            dpre += a.partial[(2 * (int64_t)k + 1) * a.channels + d];
+        }
+    sums[0][group][c] = p, sums[1][group][c] = dpre;
+    __syncthreads();
+    if (group || d >= a.channels) return;
+    for (int k = 1; k < kSumGroups; ++k) p += sums[0][k][c], dpre += sums[1][k][c];
+    if (a.dpost) a.dpost[d] = p * (a.scale ? a.scale[d] : 1.0f);
+    if (a.dscale) a.dscale[d] = p * a.post[d];
+    if (a.dpre) a.dpre[d] = dpre;
+}
+
+// Rows wider than a workgroup holds are read once for each sum and once more
+// for the results, which are written after their row's last read.
+constexpr int kWideThreads = 1024, kWideGroups = 64;
+
 template <typename E>
-struct Row {
+struct Wide {
     using T = typename E::T;
     const NormArgs &a;
     int64_t row;
     __device__ float at(const void *p, int64_t stride, int d) const { return E::to_f(((const T *)p)[row * stride + d]); }
     __device__ void put(void *p, int64_t stride, int d, float v) const { ((T *)p)[row * stride + d] = E::of_f(v); }
+    __device__ float weight(int d) const { return a.post[d] * (a.scale ? a.scale[d] : 1.0f); }
     __device__ float gate(int d, float *slope) const {
-        if (!a.z) {
-            *slope = 0.0f;
-            return 1.0f;
-        }
+        *slope = 0.0f;
+        if (!a.z) return 1.0f;
         const float z = at(a.z, a.zs, d), s = sigmoid(z), g = z * s;
         *slope = fmaf(g, 1.0f - s, s);
         return g;
     }
     __device__ float o(int d, float iy) const {
         float v = at(a.x, a.xs, d), slope;
-        if (a.y) v = fmaf(weight(a, d) * gate(d, &slope), at(a.y, a.ys, d) * iy, v);
+        if (a.y) v = fmaf(weight(d) * gate(d, &slope), at(a.y, a.ys, d) * iy, v);
         return v;
     }
-    // the gradient that reaches o
+    // the gradient that reaches o; mean: of v oh
     __device__ float t(int d, float iy, float io, float mean) const {
         float v = a.dout ? at(a.dout, a.douts, d) : 0.0f;
-        if (a.pre) v += io * (at(a.dnormed, a.dnormeds, d) * a.pre[d] * one_channel(a, io) - o(d, iy) * io * mean);
+        if (a.pre) v += io * (at(a.dnormed, a.dnormeds, d) * a.pre[d] - o(d, iy) * io * mean);
         return v;
     }
 };
 
 template <typename E>
-__global__ void __launch_bounds__(kThreads) norm_forward(NormArgs a) {
-    const Row<E> row{a, blockIdx.x};
-    float iy = 0.0f, io = 0.0f;
+__global__ void __launch_bounds__(kWideThreads) norm_forward_wide(NormArgs a) {
+    __shared__ float buffers[2][1][kWideThreads / kWave];
+    GroupSum<kWideThreads, 1> sum{buffers};
+    const Wide<E> row{a, blockIdx.x};
+    float iy = 0.0f, io = 0.0f, s[1] = {0.0f};
     if (a.y) {
-        float s = 0.0f;
-        for (int d = threadIdx.x; d < a.channels; d += kThreads) {
-            const float v = row.at(a.y, a.ys, d);
-            s = fmaf(v, v, s);
-        }
-        iy = 1.0f / sqrtf(fmaf(block_sum(s), a.inv_channels, a.eps));
+        for (int d = threadIdx.x; d < a.channels; d += kWideThreads) s[0] = fmaf(row.at(a.y, a.ys, d), row.at(a.y, a.ys, d), s[0]);
+        sum(s);
+        iy = 1.0f / sqrtf(fmaf(s[0], a.inv_channels, a.eps));
     }
     if (a.pre) {
-        float s = 0.0f;
-        for (int d = threadIdx.x; d < a.channels; d += kThreads) {
+        s[0] = 0.0f;
+        for (int d = threadIdx.x; d < a.channels; d += kWideThreads) {
             const float v = row.o(d, iy);
-            s = fmaf(v, v, s);
+            s[0] = fmaf(v, v, s[0]);
         }
-        io = 1.0f / sqrtf(fmaf(block_sum(s), a.inv_channels, a.eps));
+        sum(s);
+        io = 1.0f / sqrtf(fmaf(s[0], a.inv_channels, a.eps));
     }
-    for (int d = threadIdx.x; d < a.channels; d += kThreads) {
+    for (int d = threadIdx.x; d < a.channels; d += kWideThreads) {
         const float o = row.o(d, iy);
         if (a.out) row.put(a.out, a.outs, d, o);
         if (a.pre) row.put(a.normed, a.normeds, d, o * io * a.pre[d]);
@@ -100,72 +380,99 @@ __global__ void __launch_bounds__(kThreads) norm_forward(NormArgs a) {
     if (a.stats && threadIdx.x < 2) a.stats[2 * row.row + threadIdx.x] = threadIdx.x ? io : iy;
 }
 
-// mean(v oh) of each row
+// A workgroup's rows one after another; its sums for the weights' gradients are
+// its part of the workspace, which only it touches.
 template <typename E>
-__global__ void __launch_bounds__(kThreads) norm_row_mean(NormArgs a) {
-    const Row<E> row{a, blockIdx.x};
-    const float iy = a.stats[2 * row.row], io = a.stats[2 * row.row + 1];
-    float s = 0.0f;
-    for (int d = threadIdx.x; d < a.channels; d += kThreads)
-        s = fmaf(row.at(a.dnormed, a.dnormeds, d) * a.pre[d], row.o(d, iy) * io, s);
-    s = block_sum(s);
-    if (threadIdx.x == 0) a.mean[row.row] = a.channels == 1 ? 0.0f : s * a.inv_channels;
-}
-
-// partial sums of the weights' gradients over a group of rows
-template <typename E>
-__global__ void __launch_bounds__(kThreads) norm_columns(NormArgs a) {
-    const int d = blockIdx.x * kThreads + threadIdx.x;
-    if (d >= a.channels) return;
-    float p = 0.0f, dpre = 0.0f;
-    for (int64_t k = blockIdx.y; k < a.rows; k += gridDim.y) {
-        const Row<E> row{a, k};
+__global__ void __launch_bounds__(kWideThreads) norm_backward_wide(NormArgs a) {
+    __shared__ float buffers[2][1][kWideThreads / kWave];
+    GroupSum<kWideThreads, 1> sum{buffers};
+    float *part = a.partial + 2 * (int64_t)blockIdx.x * a.channels;
+    for (int d = threadIdx.x; d < 2 * a.channels; d += kWideThreads) part[d] = 0.0f;
+    __syncthreads();
+    for (int64_t k = blockIdx.x; k < a.rows; k += gridDim.x) {
+        const Wide<E> row{a, k};
         const float iy = a.stats[2 * k], io = a.stats[2 * k + 1];
-        float slope;
-        if (a.y) p = fmaf(row.t(d, iy, io, a.pre ? a.mean[k] : 0.0f) * row.gate(d, &slope), row.at(a.y, a.ys, d) * iy, p);
-        if (a.pre) dpre = fmaf(row.at(a.dnormed, a.dnormeds, d), row.o(d, iy) * io, dpre);
+        float s[1] = {0.0f}, mean = 0.0f, mean_y = 0.0f, slope;
+        if (a.pre) {
+            for (int d = threadIdx.x; d < a.channels; d += kWideThreads)
+                s[0] = fmaf(row.at(a.dnormed, a.dnormeds, d) * a.pre[d], row.o(d, iy) * io, s[0]);
+            sum(s);
+            mean = s[0] * a.inv_channels;
+        }
+        if (a.y) {
+            s[0] = 0.0f;
+            for (int d = threadIdx.x; d < a.channels; d += kWideThreads)
+                s[0] = fmaf(row.t(d, iy, io, mean) * row.weight(d) * row.gate(d, &slope), row.at(a.y, a.ys, d) * iy, s[0]);
+            sum(s);
+            mean_y = s[0] * a.inv_channels;
+        }
+        for (int d = threadIdx.x; d < a.channels; d += kWideThreads) {
+            const float t = row.t(d, iy, io, mean);
+            float dy = 0.0f, dz = 0.0f;
+            if (a.pre) part[a.channels + d] = fmaf(row.at(a.dnormed, a.dnormeds, d), row.o(d, iy) * io, part[a.channels + d]);
+            if (a.y) {
+                const float m = row.at(a.y, a.ys, d) * iy, tw = t * row.weight(d), gate = row.gate(d, &slope);
+                part[d] = fmaf(t * gate, m, part[d]);
+                dy = iy * (tw * gate - m * mean_y);
+                dz = tw * m * slope;
+            }
+            row.put(a.dx, a.dxs, d, t);
+            if (a.y) row.put(a.dy, a.dys, d, dy);
+            if (a.z) row.put(a.dz, a.dzs, d, dz);
+        }
     }
-    a.partial[(2 * (int64_t)blockIdx.y) * a.channels + d] = p;
-    a.partial[(2 * (int64_t)blockIdx.y + 1) * a.channels + d] = dpre;
 }
 
-__global__ void __launch_bounds__(kThreads) norm_sum_columns(NormArgs a, int groups) {
-    const int d = blockIdx.x * kThreads + threadIdx.x;
-    if (d >= a.channels) return;
-    float p = 0.0f, dpre = 0.0f;
-    for (int k = 0; k < groups; ++k) {
-        p += a.partial[(2 * (int64_t)k) * a.channels + d];
-        dpre += a.partial[(2 * (int64_t)k + 1) * a.channels + d];
+// How the rows are held: threads to a row and accesses of 16 bytes per thread.
+struct Shape {
+    int threads, accesses;
+    // two FP32 rows of weights
+    size_t lds(int type) const { return (size_t)(2 * threads * accesses) * (16 / element_bytes(type)) * sizeof(float); }
+    int at_once() const { return threads == kWave ? 4 : 1; }
+    // workgroups of one call: `most`, evened out over the rows
+    int64_t grid(int64_t rows, int64_t most) const {
+        const int64_t groups = ceil_div(rows, at_once());
+        return groups <= most ? groups : ceil_div(groups, ceil_div(groups, most));
     }
-    if (a.dpost) a.dpost[d] = p * (a.scale ? a.scale[d] : 1.0f);
-    if (a.dscale) a.dscale[d] = p * a.post[d];
-    if (a.dpre) a.dpre[d] = dpre;
+    int64_t parts(int64_t rows) const { return backward_grid(rows) * at_once(); }
+    int64_t backward_grid(int64_t rows) const { return grid(rows, threads <= 256 ? 1024 : threads == 512 ? 512 : 256); }
+    int64_t forward_grid(int64_t rows) const { return grid(rows, threads <= 256 ? 2048 : threads == 512 ? 1024 : 512); }
+};
+
+int64_t parts_of(const Shape &s, int64_t rows) {
+    return s.accesses ? s.parts(rows) : rows < kWideGroups ? rows : kWideGroups;
+}
+
+Shape shape_of(int64_t channels, int type) {
+    const int64_t v = ceil_div(channels, 16 / (int64_t)element_bytes(type));  // accesses of a row
+    if (channels > kMaxHeld) return {kWideThreads, 0};
+    if (v <= 64) return {64, 1};
+    if (v <= 128) return {64, 2};
+    if (v <= 256) return {256, 1};
+    if (v <= 512) return {256, 2};
+    if (v <= 1024) return {512, 2};
+    if (v <= 2048) return {1024, 2};
+    return {1024, 4};  // FP32 only
 }
 
 template <typename E>
-__global__ void __launch_bounds__(kThreads) norm_backward(NormArgs a) {
-    const Row<E> row{a, blockIdx.x};
-    const float iy = a.stats[2 * row.row], io = a.stats[2 * row.row + 1], mean = a.pre ? a.mean[row.row] : 0.0f;
-    float s = 0.0f, slope;
-    if (a.y) {
-        for (int d = threadIdx.x; d < a.channels; d += kThreads)
-            s = fmaf(row.t(d, iy, io, mean) * weight(a, d) * row.gate(d, &slope), row.at(a.y, a.ys, d) * iy, s);
-        s = a.channels == 1 ? 0.0f : block_sum(s) * a.inv_channels;
-    }
-    for (int d = threadIdx.x; d < a.channels; d += kThreads) {
-        const float t = row.t(d, iy, io, mean);
-        if (a.y) {
-            const float m = row.at(a.y, a.ys, d) * iy, tw = t * weight(a, d);
-            const float dy = iy * (tw * row.gate(d, &slope) * one_channel(a, iy) - m * s);
-            if (a.z) row.put(a.dz, a.dzs, d, tw * m * slope);
-            row.put(a.dy, a.dys, d, dy);
-        }
-        row.put(a.dx, a.dxs, d, t);
-    }
+const void *forward_of(const Shape &s) {
+    if (s.accesses == 0) return (const void *)norm_forward_wide<E>;
+    if (s.threads == 64) return s.accesses == 1 ? (const void *)norm_forward<E, 1, 64> : (const void *)norm_forward<E, 2, 64>;
+    if (s.threads == 256) return s.accesses == 1 ? (const void *)norm_forward<E, 1, 256> : (const void *)norm_forward<E, 2, 256>;
+    if (s.threads == 512) return (const void *)norm_forward<E, 2, 512>;
+    if (sizeof(typename E::T) == 4 && s.accesses == 4) return (const void *)norm_forward<F32, 4, 1024>;
+    return (const void *)norm_forward<E, 2, 1024>;
 }
-
-#define KERNEL_OF(type, name) \
-    ((type) == SEQ_FP32 ? (const void *)name<F32> : (type) == SEQ_FP16 ? (const void *)name<F16> : (const void *)name<BF16>)
+template <typename E>
+const void *backward_of(const Shape &s) {
+    if (s.accesses == 0) return (const void *)norm_backward_wide<E>;
+    if (s.threads == 64) return s.accesses == 1 ? (const void *)norm_backward<E, 1, 64> : (const void *)norm_backward<E, 2, 64>;
+    if (s.threads == 256) return s.accesses == 1 ? (const void *)norm_backward<E, 1, 256> : (const void *)norm_backward<E, 2, 256>;
+    if (s.threads == 512) return (const void *)norm_backward<E, 2, 512>;
+    if (sizeof(typename E::T) == 4 && s.accesses == 4) return (const void *)norm_backward<F32, 4, 1024>;
+    return (const void *)norm_backward<E, 2, 1024>;
+}
 
 bool sizes_ok(int64_t rows, int64_t channels) { return rows >= 0 && channels >= 1; }
 bool sizes_supported(int64_t rows, int64_t channels) { return rows <= kMaxSize && channels <= kMaxChannels; }
@@ -210,12 +517,15 @@ int seq_norm_forward(int64_t rows, int64_t channels, int type, const void *x, co
     a.xs = v[0].si, a.ys = v[1].si, a.zs = v[2].si, a.outs = v[3].si, a.normeds = v[4].si;
     a.post = post, a.scale = scale, a.pre = pre, a.stats = stats;
     void *args[] = {&a};
-    return launch(KERNEL_OF(type, norm_forward), dim3((unsigned)rows), dim3(kThreads), args, 0, stream);
+    const Shape s = shape_of(channels, type);
+    const void *kernel = type == SEQ_FP32 ? forward_of<F32>(s) : type == SEQ_FP16 ? forward_of<F16>(s) : forward_of<BF16>(s);
+    const int64_t groups = s.accesses ? s.forward_grid(rows) : rows;
+    return launch(kernel, dim3((unsigned)groups), dim3(s.threads * s.at_once()), args, s.lds(type), stream);
 }
 
 size_t seq_norm_workspace_bytes(int64_t rows, int64_t channels, int type) {
     if (!sizes_ok(rows, channels) || !sizes_supported(rows, channels) || !known_type(type)) return 0;
-    return up16((size_t)rows * 4) + up16((size_t)(2 * kRowGroups) * (size_t)channels * 4);
+    return up16((size_t)(2 * parts_of(shape_of(channels, type), rows)) * (size_t)channels * 4);
 }
 
 int seq_norm_backward(int64_t rows, int64_t channels, int type, const void *dout, const void *dnormed,
@@ -258,18 +568,19 @@ int seq_norm_backward(int64_t rows, int64_t channels, int type, const void *dout
     a.douts = v[0].si, a.dnormeds = v[1].si, a.xs = v[2].si, a.ys = v[3].si, a.zs = v[4].si;
     a.dxs = v[5].si, a.dys = v[6].si, a.dzs = v[7].si;
     a.post = post, a.scale = scale, a.pre = pre, a.stats = const_cast<float *>(stats);
-    a.mean = (float *)workspace, a.partial = (float *)((char *)workspace + up16((size_t)rows * 4));
+    a.partial = (float *)workspace;
     a.dpost = dpost, a.dscale = dscale, a.dpre = dpre;
-    int groups = rows ? kRowGroups : 0;
-    void *args[] = {&a, &groups};
-    const dim3 block(kThreads);
-    const unsigned columns = (unsigned)ceil_div(channels, kThreads);
-    int rc = SEQ_OK;
-    if (rows && pre) rc = launch(KERNEL_OF(type, norm_row_mean), dim3((unsigned)rows), block, args, 0, stream);
-    if (rc == SEQ_OK && rows) rc = launch(KERNEL_OF(type, norm_columns), dim3(columns, kRowGroups), block, args, 0, stream);
-    if (rc == SEQ_OK) rc = launch((const void *)norm_sum_columns, dim3(columns), block, args, 0, stream);
-    if (rc == SEQ_OK && rows) rc = launch(KERNEL_OF(type, norm_backward), dim3((unsigned)rows), block, args, 0, stream);
-    return rc;
+    const Shape s = shape_of(channels, type);
+    int parts = (int)parts_of(s, rows);
+    void *args[] = {&a, &parts};
+    if (rows) {
+        const void *kernel = type == SEQ_FP32 ? backward_of<F32>(s) : type == SEQ_FP16 ? backward_of<F16>(s) : backward_of<BF16>(s);
+        const int64_t groups = s.accesses ? s.backward_grid(rows) : parts;
+        const int rc = launch(kernel, dim3((unsigned)groups), dim3(s.threads * s.at_once()), args, s.lds(type), stream);
+        if (rc != SEQ_OK) return rc;
+    }
+    return launch((const void *)norm_sum, dim3((unsigned)ceil_div(channels, kSumChannels)), dim3(kSumChannels * kSumGroups), args, 0,
+                  stream);
 }
 
 }  // extern "C"

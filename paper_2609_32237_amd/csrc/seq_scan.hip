@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kWave *W) scan_forward(ScanArgs a) {
                     out[j] = full || s < k.count ? h[j] : 0.0f;
                 }
                 Pack<E, V> p;
-                p.set(out);
+                p.set(0, out);
                 if (k.live) p.store(y + s * a.yt + k.at);
             }
     };
@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(kWave *W) scan_backward(ScanArgs a) {
                     }
                 }
                 Pack<E, V> ax, ar, ag;
-                ax.set(ox), ar.set(orr), ag.set(og);
+                ax.set(0, ox), ar.set(0, orr), ag.set(0, og);
                 if (k.live) {
                     ax.store(dx + s * a.dxt + k.at);
                     ar.store(dr + s * a.drt + k.at);
