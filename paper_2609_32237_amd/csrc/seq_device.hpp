@@ -58,19 +58,32 @@ __device__ __forceinline__ float sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * v));
 }
 
-// Sum over the wave, the same in every lane: 4 steps of cross-lane moves make
-// the sums of 16 lanes, four of those are read to scalar registers.
-__device__ __forceinline__ float wave_sum(float v) {
+// Sum over groups of WIDTH (4, 8 or 16) lanes that follow each other, in every
+// lane, by moves between the lanes of 16; for 4 and 8 the 16 lanes hold the
+// same groups.
+template <int WIDTH>
+__device__ __forceinline__ float lanes_sum(float v) {
     auto moved = [](float x, auto ctrl) {
         return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
     };
-    v += moved(v, std::integral_constant<int, 0xb1>{});   // lanes 1 0 3 2 of each four
-    v += moved(v, std::integral_constant<int, 0x4e>{});   // lanes 2 3 0 1
-    v += moved(v, std::integral_constant<int, 0x124>{});  // rotated by 4 within 16
-    v += moved(v, std::integral_constant<int, 0x128>{});  // rotated by 8
+    v += moved(v, std::integral_constant<int, 0xb1>{});                         // lanes 1 0 3 2 of each four
+    v += moved(v, std::integral_constant<int, 0x4e>{});                         // lanes 2 3 0 1
+    if (WIDTH > 4) v += moved(v, std::integral_constant<int, 0x124>{});   // rotated by 4 within 16
+    if (WIDTH > 8) v += moved(v, std::integral_constant<int, 0x128>{});   // rotated by 8
+    return v;
+}
+
+// Sum over the wave, the same in every lane: the sums of 16 lanes, four of
+// which are read to scalar registers.
+__device__ __forceinline__ float wave_sum(float v) {
+    v = lanes_sum<16>(v);
     auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
     return (lane(0) + lane(16)) + (lane(32) + lane(48));
 }
+
+// Has a value computed here: left alone, the compiler moves work behind the
+// next branch, and holds all of its inputs instead of the result.
+__device__ __forceinline__ void pin(float &v) { asm volatile("" : "+v"(v)); }
 
 // V consecutive elements in one access of up to 16 bytes.  Accesses need no
 // more than element alignment: the hardware takes them at any address.
@@ -96,29 +109,45 @@ struct Pack {
 
     __device__ __forceinline__ void load(const T *p) { u = ((const Unaligned *)p)->u; }
     __device__ __forceinline__ void store(T *p) const { ((Unaligned *)p)->u = u; }
+    // `past`: past the caches, for results too large to be found there again
+    __device__ __forceinline__ void store(T *p, bool past) const {
+        if (past)
+            __builtin_nontemporal_store(u, &((Unaligned *)p)->u);
+        else
+            store(p);
+    }
     // Keeps the stored form: what was converted from it before is converted
     // again after this, instead of being held in twice the registers.
     __device__ __forceinline__ void hold() { asm volatile("" : "+v"(u)); }
-    // elements `at` .. of a row of `end`, zeros behind it
-    __device__ __forceinline__ void load(const T *row, int at, int end) {
-        if (at + V <= end) {
-            load(row + at);
+    // Elements `at` .. of a row of `end`, zeros behind it.  The row's address is
+    // the same in every lane, and an unsigned 32-bit offset of bytes from it needs
+    // no 64-bit address in vector registers.  WHOLE: `end` is a multiple of V.
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const T *row, unsigned at, unsigned end) {
+        const char *p = (const char *)row;
+        if (WHOLE) {
+            load((const T *)(p + (at < end ? at : end - V) * (unsigned)sizeof(T)));
+            u = at < end ? u : U{};
+        } else if (at + V <= end) {
+            load((const T *)(p + at * (unsigned)sizeof(T)));
         } else {
             T v[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = at + j < end ? row[at + j] : (T)0.0f;
+            for (int j = 0; j < V; ++j) v[j] = at + j < end ? ((const T *)(p + at * (unsigned)sizeof(T)))[j] : (T)0.0f;
             __builtin_memcpy(&u, v, sizeof(u));
         }
     }
-    __device__ __forceinline__ void store(T *row, int at, int end) const {
-        if (at + V <= end) {
-            store(row + at);
-        } else {
+    template <bool WHOLE>
+    __device__ __forceinline__ void store(T *row, unsigned at, unsigned end, bool past) const {
+        T *p = (T *)((char *)row + at * (unsigned)sizeof(T));
+        if (WHOLE ? at < end : at + V <= end) {
+            store(p, past);
+        } else if (!WHOLE) {
             T v[V];
             __builtin_memcpy(v, &u, sizeof(u));
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (at + j < end) row[at + j] = v[j];
+                if (at + j < end) p[j] = v[j];
         }
     }
     // the word that holds element j of a 16-bit pack

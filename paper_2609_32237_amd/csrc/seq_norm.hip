@@ -20,6 +20,7 @@ struct NormArgs {
     int64_t xs, ys, zs, outs, normeds, douts, dnormeds, dxs, dys, dzs;
     const float *post, *scale, *pre;
     float *stats, *partial, *dpost, *dscale, *dpre;
+    int stream_out;  // results past the caches
 };
 
 // v - vh mean(v vh) of a row vh of norm 1 - eps i^2: with one channel it is
@@ -47,11 +48,7 @@ struct GroupSum {
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            v[i] = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) v[i] += part[i][w];
-        }
+        for (int i = 0; i < COUNT; ++i) v[i] = lanes_sum<kWaves>(part[i][threadIdx.x % kWaves]);
         turn ^= 1;
     }
 };
@@ -64,28 +61,28 @@ struct GroupSum {
 template <int THREADS>
 constexpr int kRowsAtOnce = THREADS == kWave ? 4 : 1;
 
-template <typename E, int N, int THREADS>
+template <typename E, int N, int THREADS, bool WHOLE>
 struct Held {
     using T = typename E::T;
     static constexpr int V = 16 / sizeof(T);
     static constexpr int kWeights = N * THREADS * V;  // floats of LDS for one row of weights
     using P = Pack<E, V>;
-    int lane, end;
+    unsigned lane, end;
 
     __device__ __forceinline__ explicit Held(int channels) : lane(threadIdx.x % THREADS), end(channels) {}
     // first channel of access n
-    __device__ __forceinline__ int at(int n) const { return (n * THREADS + lane) * V; }
+    __device__ __forceinline__ unsigned at(int n) const { return (n * THREADS + lane) * V; }
     // a row of an activation; zeros where there is none
     __device__ __forceinline__ void load(P (&p)[N], const void *base, int64_t row, int64_t stride) const {
         const T *r = (const T *)base + row * stride;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             p[n].u = typename P::U{};
-            if (base) p[n].load(r, at(n), end);
+            if (base) p[n].template load<WHOLE>(r, at(n), end);
         }
     }
-    __device__ __forceinline__ void store(const P &p, int n, void *base, int64_t row, int64_t stride) const {
-        p.store((T *)base + row * stride, at(n), end);
+    __device__ __forceinline__ void store(const P &p, int n, void *base, int64_t row, int64_t stride, bool past) const {
+        p.template store<WHOLE>((T *)base + row * stride, at(n), end, past);
     }
     // a row of weights (times another one) into LDS; zeros where there is none
     __device__ __forceinline__ void keep(float *lds, const float *of, const float *times) const {
@@ -93,42 +90,53 @@ struct Held {
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int d = at(n) + j;
+                const unsigned d = at(n) + j;
                 float w = 0.0f;
                 if (of && d < end) w = times ? of[d] * times[d] : of[d];
                 lds[((n * (V / 4) + j / 4) * THREADS + lane) * 4 + j % 4] = w;
             }
     }
-    // four weights of access n, from 4 q on
-    __device__ __forceinline__ void weights(float (&w)[4], const float *lds, int n, int q) const {
-        const float4 f = *(const float4 *)(lds + ((n * (V / 4) + q) * THREADS + lane) * 4);
-        w[0] = f.x, w[1] = f.y, w[2] = f.z, w[3] = f.w;
+    // weights COUNT i .. COUNT i + COUNT - 1 of access n
+    template <int COUNT>
+    __device__ __forceinline__ void weights(float (&w)[COUNT], const float *lds, int n, int i) const {
+        using F = float __attribute__((ext_vector_type(COUNT)));
+        const F f = *(const F *)(lds + ((n * (V / 4) + COUNT * i / 4) * THREADS + lane) * 4 + COUNT * i % 4);
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) w[k] = f[k];
     }
 };
 
-template <typename E, int N, int THREADS>
+template <typename E, int N, int THREADS, bool WHOLE>
 __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_forward(NormArgs a) {
-    using R = Held<E, N, THREADS>;
+    using R = Held<E, N, THREADS, WHOLE>;
     constexpr int V = R::V;
     extern __shared__ float4 lds[];
     __shared__ float buffers[2][1][THREADS / kWave];
     float *lw = (float *)lds, *lpre = lw + R::kWeights;
     GroupSum<THREADS, 1> sum{buffers};
     const R at(a.channels);
+    const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<THREADS>;
+    int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<THREADS>;
+    if (THREADS == kWave) row += __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    // a row ahead: its loads are under way while the one before is worked on
+    typename R::P nx[N], ny[N], nz[N];
+    auto fetch = [&](int64_t r) {
+        at.load(ny, a.y, r, a.ys);
+        at.load(nx, a.x, r, a.xs);
+        at.load(nz, a.z, r, a.zs);
+    };
+    if (row < a.rows) fetch(row);
     if (threadIdx.x < THREADS) {
         at.keep(lw, a.post, a.scale);
         at.keep(lpre, a.pre, nullptr);
     }
     __syncthreads();
     const bool has_z = a.z != nullptr;
-    const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<THREADS>;
-    int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<THREADS>;
-    if (THREADS == kWave) row += __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     for (; row < a.rows; row += step) {
         typename R::P px[N], py[N], pz[N];
-        at.load(py, a.y, row, a.ys);
-        at.load(px, a.x, row, a.xs);
-        at.load(pz, a.z, row, a.zs);
+#pragma unroll
+        for (int n = 0; n < N; ++n) px[n] = nx[n], py[n] = ny[n], pz[n] = nz[n];
+        if (row + step < a.rows) fetch(row + step);
         float o[N][V], iy = 0.0f, io = 0.0f;
         if (a.y) {
             float s[1] = {0.0f};
@@ -159,7 +167,7 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_forward(No
                 }
                 p.set(i, f);
             }
-            if (a.out) at.store(p, n, a.out, row, a.outs);
+            if (a.out) at.store(p, n, a.out, row, a.outs, a.stream_out);
         }
         if (a.pre) {
             sum(s);
@@ -175,7 +183,7 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_forward(No
                     for (int k = 0; k < 4; ++k) pre[k] *= o[n][4 * i + k] * io;
                     p.set(i, pre);
                 }
-                at.store(p, n, a.normed, row, a.normeds);
+                at.store(p, n, a.normed, row, a.normeds, a.stream_out);
             }
         }
         if (a.stats && at.lane < 2) a.stats[2 * row + at.lane] = at.lane ? io : iy;
@@ -188,37 +196,52 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_forward(No
 //     mean(t p) = mean((dout + v / rms(o)) p) - mean(v oh) / rms(o) mean(oh p).
 // The sums for the weights' gradients stay in each lane's registers over its
 // rows; every workgroup writes its own, and norm_sum joins them in order.
-template <typename E, int N, int THREADS>
+template <typename E, int N, int THREADS, bool WHOLE>
 __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(NormArgs a) {
-    using R = Held<E, N, THREADS>;
+    using R = Held<E, N, THREADS, WHOLE>;
     constexpr int V = R::V;
     extern __shared__ float4 lds[];
     __shared__ float buffers[2][3][THREADS / kWave];
     float *lw = (float *)lds, *lpre = lw + R::kWeights;
     GroupSum<THREADS, 3> sum{buffers};
     const R at(a.channels);
+    const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<THREADS>;
+    int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<THREADS>;
+    if (THREADS == kWave) row += __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    // a row ahead where the registers are enough
+    constexpr bool kAhead = N * V <= 8;
+    typename R::P nx[N], ny[N], nz[N], no[N], nn[N];
+    float niy = 0.0f, nio = 0.0f;
+    auto fetch = [&](int64_t r) {
+        niy = a.stats[2 * r], nio = a.stats[2 * r + 1];
+        at.load(nx, a.x, r, a.xs);
+        at.load(ny, a.y, r, a.ys);
+        at.load(nz, a.z, r, a.zs);
+        at.load(nn, a.dnormed, r, a.dnormeds);
+        at.load(no, a.dout, r, a.douts);
+    };
+    if (kAhead && row < a.rows) fetch(row);
     if (threadIdx.x < THREADS) {
         at.keep(lw, a.post, a.scale);
         at.keep(lpre, a.pre, nullptr);
     }
     __syncthreads();
     const bool has_z = a.z != nullptr, has_pre = a.pre != nullptr;
+    // Channels taken at a time, in order: all at once, the conversions alone
+    // would fill the registers.
+    constexpr int G = 4;
     float dw[N][V], dpre[N][V];
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int j = 0; j < V; ++j) dw[n][j] = dpre[n][j] = 0.0f;
-    const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<THREADS>;
-    int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<THREADS>;
-    if (THREADS == kWave) row += __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     for (; row < a.rows; row += step) {
+        if (!kAhead) fetch(row);
         typename R::P px[N], py[N], pz[N], po[N], pn[N];
-        const float iy = a.stats[2 * row], io = a.stats[2 * row + 1];
-        at.load(px, a.x, row, a.xs);
-        at.load(py, a.y, row, a.ys);
-        at.load(pz, a.z, row, a.zs);
-        at.load(pn, a.dnormed, row, a.dnormeds);
-        at.load(po, a.dout, row, a.douts);
+        const float iy = niy, io = nio;
+#pragma unroll
+        for (int n = 0; n < N; ++n) px[n] = nx[n], py[n] = ny[n], pz[n] = nz[n], po[n] = no[n], pn[n] = nn[n];
+        if (kAhead && row + step < a.rows) fetch(row + step);
         float sg[N][V], s[3] = {0.0f, 0.0f, 0.0f};
         // of one element: o, the gate, m
         auto forward = [&](int n, int j, float w, float &gate, float &m) {
@@ -227,18 +250,16 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(N
             const float o = fmaf(w * gate, m, px[n].get(j));
             return o;
         };
-        // Four channels at a time, in this order: taken all at once, the
-        // conversions alone would fill the registers.
 #pragma unroll
         for (int n = 0; n < N; ++n) {
 #pragma unroll
-            for (int i = 0; i < V / 4; ++i) {
-                float w[4], pre[4];
+            for (int i = 0; i < V / G; ++i) {
+                float w[G], pre[G];
                 at.weights(w, lw, n, i);
                 at.weights(pre, lpre, n, i);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int j = 4 * i + k;
+                for (int k = 0; k < G; ++k) {
+                    const int j = G * i + k;
                     sg[n][j] = sigmoid(pz[n].get(j));
                     float gate, m;
                     const float oh = forward(n, j, w[k], gate, m) * io, p = w[k] * gate * m, v = pn[n].get(j) * pre[k];
@@ -259,18 +280,19 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(N
         for (int n = 0; n < N; ++n) {
             typename R::P gx, gy, gz;
 #pragma unroll
-            for (int i = 0; i < V / 4; ++i) {
-                float w[4], pre[4], dx[4], dy[4], dz[4];
+            for (int i = 0; i < V / G; ++i) {
+                float w[G], pre[G], dx[G], dy[G], dz[G];
                 at.weights(w, lw, n, i);
                 at.weights(pre, lpre, n, i);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int j = 4 * i + k;
+                for (int k = 0; k < G; ++k) {
+                    const int j = G * i + k;
                     float gate, m;
                     const float oh = forward(n, j, w[k], gate, m) * io, dn = pn[n].get(j);
                     dpre[n][j] = fmaf(dn, oh, dpre[n][j]);
                     const float t = po[n].get(j) + (has_pre ? fo * (dn * pre[k]) - mean * oh : 0.0f), tw = t * w[k];
                     dw[n][j] = fmaf(t * gate, m, dw[n][j]);
+                    pin(dw[n][j]), pin(dpre[n][j]);
                     dx[k] = t;
                     dy[k] = iy * (tw * gate * fy - m * mean_y);
                     dz[k] = tw * m * fmaf(gate, 1.0f - sg[n][j], sg[n][j]);
@@ -278,11 +300,12 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(N
                 gx.set(i, dx);
                 gy.set(i, dy);
                 gz.set(i, dz);
+                gx.hold(), gy.hold(), gz.hold();
                 __builtin_amdgcn_sched_barrier(0);
             }
-            at.store(gx, n, a.dx, row, a.dxs);
-            if (a.y) at.store(gy, n, a.dy, row, a.dys);
-            if (a.z) at.store(gz, n, a.dz, row, a.dzs);
+            at.store(gx, n, a.dx, row, a.dxs, a.stream_out);
+            if (a.y) at.store(gy, n, a.dy, row, a.dys, a.stream_out);
+            if (a.z) at.store(gz, n, a.dz, row, a.dzs, a.stream_out);
         }
     }
     // this workgroup's (for short rows: this wave's) part of the weights' gradients
@@ -293,31 +316,34 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(N
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            if (at.at(n) + j < a.channels) {
+            if (at.at(n) + j < at.end) {
                 part[at.at(n) + j] = dw[n][j];
-                part[a.channels + at.at(n) + j] = dpre[n][j];
+                part[at.end + at.at(n) + j] = dpre[n][j];
             }
 }
 
-// The weights' gradients from the parts: 32 channels to a workgroup, 32 groups
-// of parts joined in order.
-constexpr int kSumChannels = 32, kSumGroups = 32;
+// The weights' gradients from the parts, one of the two sums in each half of the
+// grid: 16 channels to a workgroup, 64 groups of parts joined in order.
+constexpr int kSumChannels = 16, kSumGroups = 64;
 __global__ void __launch_bounds__(kSumChannels *kSumGroups) norm_sum(NormArgs a, int parts) {
-    __shared__ float sums[2][kSumGroups][kSumChannels];
+    __shared__ float sums[kSumGroups][kSumChannels];
     const int c = threadIdx.x % kSumChannels, group = threadIdx.x / kSumChannels, d = blockIdx.x * kSumChannels + c;
-    float p = 0.0f, dpre = 0.0f;
-    if (d < a.channels)
-        for (int k = group; k < parts; k += kSumGroups) {
-            p += a.partial[2 * (int64_t)k * a.channels + d];
-            dpre += a.partial[(2 * (int64_t)k + 1) * a.channels + d];
-        }
-    sums[0][group][c] = p, sums[1][group][c] = dpre;
+    const float *part = a.partial + (int64_t)blockIdx.y * a.channels + d;
+    float s = 0.0f;
+    if (d < a.channels) {
+#pragma unroll 4
+        for (int k = group; k < parts; k += kSumGroups) s += part[2 * (int64_t)k * a.channels];
+    }
+    sums[group][c] = s;
     __syncthreads();
     if (group || d >= a.channels) return;
-    for (int k = 1; k < kSumGroups; ++k) p += sums[0][k][c], dpre += sums[1][k][c];
-    if (a.dpost) a.dpost[d] = p * (a.scale ? a.scale[d] : 1.0f);
-    if (a.dscale) a.dscale[d] = p * a.post[d];
-    if (a.dpre) a.dpre[d] = dpre;
+    for (int k = 1; k < kSumGroups; ++k) s += sums[k][c];
+    if (blockIdx.y) {
+        if (a.dpre) a.dpre[d] = s;
+        return;
+    }
+    if (a.dpost) a.dpost[d] = s * (a.scale ? a.scale[d] : 1.0f);
+    if (a.dscale) a.dscale[d] = s * a.post[d];
 }
 
 // Rows wider than a workgroup holds are read once for each sum and once more
@@ -455,24 +481,36 @@ Shape shape_of(int64_t channels, int type) {
     return {1024, 4};  // FP32 only
 }
 
-template <typename E>
-const void *forward_of(const Shape &s) {
-    if (s.accesses == 0) return (const void *)norm_forward_wide<E>;
-    if (s.threads == 64) return s.accesses == 1 ? (const void *)norm_forward<E, 1, 64> : (const void *)norm_forward<E, 2, 64>;
-    if (s.threads == 256) return s.accesses == 1 ? (const void *)norm_forward<E, 1, 256> : (const void *)norm_forward<E, 2, 256>;
-    if (s.threads == 512) return (const void *)norm_forward<E, 2, 512>;
-    if (sizeof(typename E::T) == 4 && s.accesses == 4) return (const void *)norm_forward<F32, 4, 1024>;
-    return (const void *)norm_forward<E, 2, 1024>;
+template <bool BACK, typename E, int N, int THREADS>
+const void *held_of(bool whole) {
+    if constexpr (BACK)
+        return whole ? (const void *)norm_backward<E, N, THREADS, true> : (const void *)norm_backward<E, N, THREADS, false>;
+    else
+        return whole ? (const void *)norm_forward<E, N, THREADS, true> : (const void *)norm_forward<E, N, THREADS, false>;
 }
-template <typename E>
-const void *backward_of(const Shape &s) {
-    if (s.accesses == 0) return (const void *)norm_backward_wide<E>;
-    if (s.threads == 64) return s.accesses == 1 ? (const void *)norm_backward<E, 1, 64> : (const void *)norm_backward<E, 2, 64>;
-    if (s.threads == 256) return s.accesses == 1 ? (const void *)norm_backward<E, 1, 256> : (const void *)norm_backward<E, 2, 256>;
-    if (s.threads == 512) return (const void *)norm_backward<E, 2, 512>;
-    if (sizeof(typename E::T) == 4 && s.accesses == 4) return (const void *)norm_backward<F32, 4, 1024>;
-    return (const void *)norm_backward<E, 2, 1024>;
+template <bool BACK, typename E>
+const void *kernel_of(const Shape &s, int64_t channels) {
+    if (s.accesses == 0) {
+        if constexpr (BACK)
+            return (const void *)norm_backward_wide<E>;
+        else
+            return (const void *)norm_forward_wide<E>;
+    }
+    const bool whole = channels % (16 / sizeof(typename E::T)) == 0;
+    if (s.threads == 64) return s.accesses == 1 ? held_of<BACK, E, 1, 64>(whole) : held_of<BACK, E, 2, 64>(whole);
+    if (s.threads == 256) return s.accesses == 1 ? held_of<BACK, E, 1, 256>(whole) : held_of<BACK, E, 2, 256>(whole);
+    if (s.threads == 512) return held_of<BACK, E, 2, 512>(whole);
+    if constexpr (sizeof(typename E::T) == 4)
+        if (s.accesses == 4) return held_of<BACK, E, 4, 1024>(whole);
+    return held_of<BACK, E, 2, 1024>(whole);
 }
+template <bool BACK>
+const void *kernel_of(const Shape &s, int64_t channels, int type) {
+    return type == SEQ_FP32 ? kernel_of<BACK, F32>(s, channels) : type == SEQ_FP16 ? kernel_of<BACK, F16>(s, channels) : kernel_of<BACK, BF16>(s, channels);
+}
+
+// Outputs of this many bytes are written past the caches.
+constexpr int64_t kStreamBytes = int64_t(16) << 20;
 
 bool sizes_ok(int64_t rows, int64_t channels) { return rows >= 0 && channels >= 1; }
 bool sizes_supported(int64_t rows, int64_t channels) { return rows <= kMaxSize && channels <= kMaxChannels; }
@@ -518,9 +556,9 @@ int seq_norm_forward(int64_t rows, int64_t channels, int type, const void *x, co
     a.post = post, a.scale = scale, a.pre = pre, a.stats = stats;
     void *args[] = {&a};
     const Shape s = shape_of(channels, type);
-    const void *kernel = type == SEQ_FP32 ? forward_of<F32>(s) : type == SEQ_FP16 ? forward_of<F16>(s) : forward_of<BF16>(s);
+    a.stream_out = rows * channels >= kStreamBytes / (int64_t)grid.bytes;
     const int64_t groups = s.accesses ? s.forward_grid(rows) : rows;
-    return launch(kernel, dim3((unsigned)groups), dim3(s.threads * s.at_once()), args, s.lds(type), stream);
+    return launch(kernel_of<false>(s, channels, type), dim3((unsigned)groups), dim3(s.threads * s.at_once()), args, s.lds(type), stream);
 }
 
 size_t seq_norm_workspace_bytes(int64_t rows, int64_t channels, int type) {
@@ -574,12 +612,12 @@ int seq_norm_backward(int64_t rows, int64_t channels, int type, const void *dout
     int parts = (int)parts_of(s, rows);
     void *args[] = {&a, &parts};
     if (rows) {
-        const void *kernel = type == SEQ_FP32 ? backward_of<F32>(s) : type == SEQ_FP16 ? backward_of<F16>(s) : backward_of<BF16>(s);
+        a.stream_out = rows * channels >= kStreamBytes / (int64_t)grid.bytes;
         const int64_t groups = s.accesses ? s.backward_grid(rows) : parts;
-        const int rc = launch(kernel, dim3((unsigned)groups), dim3(s.threads * s.at_once()), args, s.lds(type), stream);
+        const int rc = launch(kernel_of<true>(s, channels, type), dim3((unsigned)groups), dim3(s.threads * s.at_once()), args, s.lds(type), stream);
         if (rc != SEQ_OK) return rc;
     }
-    return launch((const void *)norm_sum, dim3((unsigned)ceil_div(channels, kSumChannels)), dim3(kSumChannels * kSumGroups), args, 0,
+    return launch((const void *)norm_sum, dim3((unsigned)ceil_div(channels, kSumChannels), 2), dim3(kSumChannels * kSumGroups), args, 0,
                   stream);
 }
 
