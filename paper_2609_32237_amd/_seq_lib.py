@@ -7,6 +7,7 @@ importing this module fails.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -66,6 +67,9 @@ def seq_strerror(code: int) -> str:
     return lib.seq_strerror(code).decode()
 
 
+_array_of = functools.lru_cache(maxsize=None)(lambda n: ctypes.c_int64 * n)
+
+
 def int64s(values):
     """A host array of 64-bit strides."""
-    return (ctypes.c_int64 * len(values))(*values)
+    return _array_of(len(values))(*values)

@@ -84,16 +84,21 @@ struct Held {
     __device__ __forceinline__ void store(const P &p, int n, void *base, int64_t row, int64_t stride, bool past) const {
         p.template store<WHOLE>((T *)base + row * stride, at(n), end, past);
     }
-    // a row of weights (times another one) into LDS; zeros where there is none
+    // a row of weights (times another one) into LDS, four at a time; zeros where there is none
     __device__ __forceinline__ void keep(float *lds, const float *of, const float *times) const {
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const unsigned d = at(n) + j;
-                float w = 0.0f;
-                if (of && d < end) w = times ? of[d] * times[d] : of[d];
-                lds[((n * (V / 4) + j / 4) * THREADS + lane) * 4 + j % 4] = w;
+            for (int q = 0; q < V / 4; ++q) {
+                Pack<F32, 4> w, s;
+                w.u = Pack<F32, 4>::U{};
+                if (of) w.template load<WHOLE>(of, at(n) + 4 * q, end);
+                if (times) s.template load<WHOLE>(times, at(n) + 4 * q, end);
+                float f[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f[k] = times ? w.get(k) * s.get(k) : w.get(k);
+                w.set(0, f);
+                *(Pack<F32, 4>::U *)(lds + ((n * (V / 4) + q) * THREADS + lane) * 4) = w.u;
             }
     }
     // weights COUNT i .. COUNT i + COUNT - 1 of access n
@@ -208,19 +213,6 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(N
     const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<THREADS>;
     int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<THREADS>;
     if (THREADS == kWave) row += __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    // a row ahead where the registers are enough
-    constexpr bool kAhead = N * V <= 8;
-    typename R::P nx[N], ny[N], nz[N], no[N], nn[N];
-    float niy = 0.0f, nio = 0.0f;
-    auto fetch = [&](int64_t r) {
-        niy = a.stats[2 * r], nio = a.stats[2 * r + 1];
-        at.load(nx, a.x, r, a.xs);
-        at.load(ny, a.y, r, a.ys);
-        at.load(nz, a.z, r, a.zs);
-        at.load(nn, a.dnormed, r, a.dnormeds);
-        at.load(no, a.dout, r, a.douts);
-    };
-    if (kAhead && row < a.rows) fetch(row);
     if (threadIdx.x < THREADS) {
         at.keep(lw, a.post, a.scale);
         at.keep(lpre, a.pre, nullptr);
@@ -236,12 +228,13 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(N
 #pragma unroll
         for (int j = 0; j < V; ++j) dw[n][j] = dpre[n][j] = 0.0f;
     for (; row < a.rows; row += step) {
-        if (!kAhead) fetch(row);
         typename R::P px[N], py[N], pz[N], po[N], pn[N];
-        const float iy = niy, io = nio;
-#pragma unroll
-        for (int n = 0; n < N; ++n) px[n] = nx[n], py[n] = ny[n], pz[n] = nz[n], po[n] = no[n], pn[n] = nn[n];
-        if (kAhead && row + step < a.rows) fetch(row + step);
+        const float iy = a.stats[2 * row], io = a.stats[2 * row + 1];
+        at.load(px, a.x, row, a.xs);
+        at.load(py, a.y, row, a.ys);
+        at.load(pz, a.z, row, a.zs);
+        at.load(pn, a.dnormed, row, a.dnormeds);
+        at.load(po, a.dout, row, a.douts);
         float sg[N][V], s[3] = {0.0f, 0.0f, 0.0f};
         // of one element: o, the gate, m
         auto forward = [&](int n, int j, float w, float &gate, float &m) {
@@ -315,16 +308,23 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(N
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (at.at(n) + j < at.end) {
-                part[at.at(n) + j] = dw[n][j];
-                part[at.end + at.at(n) + j] = dpre[n][j];
-            }
+        for (int i = 0; i < V / 4; ++i) {
+            Pack<F32, 4> p;
+            float f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[k] = dw[n][4 * i + k];
+            p.set(0, f);
+            p.template store<WHOLE>(part, at.at(n) + 4 * i, at.end, false);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[k] = dpre[n][4 * i + k];
+            p.set(0, f);
+            p.template store<WHOLE>(part + a.channels, at.at(n) + 4 * i, at.end, false);
+        }
 }
 
 // The weights' gradients from the parts, one of the two sums in each half of the
-// grid: 16 channels to a workgroup, 64 groups of parts joined in order.
-constexpr int kSumChannels = 16, kSumGroups = 64;
+// grid: 32 channels to a workgroup, 32 groups of parts joined in order.
+constexpr int kSumChannels = 32, kSumGroups = 32;
 __global__ void __launch_bounds__(kSumChannels *kSumGroups) norm_sum(NormArgs a, int parts) {
     __shared__ float sums[kSumGroups][kSumChannels];
     const int c = threadIdx.x % kSumChannels, group = threadIdx.x / kSumChannels, d = blockIdx.x * kSumChannels + c;

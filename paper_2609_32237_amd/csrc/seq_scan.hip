@@ -162,35 +162,44 @@ struct Tile {
     }
 };
 
-// One token: nothing to chain, a lane takes 16 bytes of each activation.
-template <typename E>
+// One token: nothing to chain, a lane takes four channels.
+constexpr int kStepChannels = 4;
+
+template <typename E, bool WHOLE>
 __global__ void __launch_bounds__(256) scan_step(ScanArgs a, unsigned per_row, unsigned items) {
     using T = typename E::T;
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = kStepChannels;
     const unsigned i = blockIdx.x * 256 + threadIdx.x;
     if (i >= items) return;
     const unsigned b = i / per_row, at = (i - b * per_row) * V, end = (unsigned)a.channels;
-    const bool counts = valid_tokens(a, b) > 0;
     Pack<E, V> x, r, g;
+    Pack<F32, V> rate, state;
+    r.template load<WHOLE>((const T *)a.r + b * a.rb, at, end);
+    g.template load<WHOLE>((const T *)a.g + b * a.gb, at, end);
+    x.template load<WHOLE>((const T *)a.x + b * a.xb, at, end);
+    rate.template load<WHOLE>(a.rate, at, end);
+    state.u = Pack<F32, V>::U{};
+    const int64_t row = (int64_t)b * a.channels;
+    if (a.state) state.template load<WHOLE>(a.state + row, at, end);
+    if (a.saved) state.template store<WHOLE>(a.saved + row, at, end, false);
+    const bool counts = valid_tokens(a, b) > 0;
     float h[V], out[V];
-    r.template load<false>((const T *)a.r + b * a.rb, at, end);
-    g.template load<false>((const T *)a.g + b * a.gb, at, end);
-    x.template load<false>((const T *)a.x + b * a.xb, at, end);
-    const int64_t state = (int64_t)b * a.channels + at;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        if (at + j >= end) continue;
-        h[j] = a.state ? a.state[state + j] : 0.0f;
-        if (a.saved) a.saved[state + j] = h[j];
-        out[j] = 0.0f;
-        if (counts) {
-            const float q = a.rate[at + j] * sigmoid(r.get(j)), c = sigmoid(g.get(j)) * x.get(j);
-            out[j] = h[j] = fmaf(q, c - h[j], h[j]);
-        }
-        if (a.state_out) a.state_out[state + j] = h[j];
+        const float q = rate.get(j) * sigmoid(r.get(j)), c = sigmoid(g.get(j)) * x.get(j);
+        h[j] = state.get(j);
+        if (counts) h[j] = fmaf(q, c - h[j], h[j]);
+        out[j] = counts ? h[j] : 0.0f;
     }
     x.set(0, out);
-    x.template store<false>((T *)a.y + b * a.yb, at, end, false);
+    x.template store<WHOLE>((T *)a.y + b * a.yb, at, end, false);
+    state.set(0, h);
+    if (a.state_out) state.template store<WHOLE>(a.state_out + row, at, end, false);
+}
+
+template <typename E>
+const void *step_kernel(int64_t channels) {
+    return channels % kStepChannels == 0 ? (const void *)scan_step<E, true> : (const void *)scan_step<E, false>;
 }
 
 template <typename E, int V, int W, bool CHAIN>
@@ -641,13 +650,11 @@ int seq_scan_forward(int64_t batch, int64_t len, int64_t channels, int type, con
     const Cut c = cut_of(batch, len, channels, type, false);
     const int rc = start(a, c, type, workspace, stream);
     if (rc != SEQ_OK) return rc;
-    // 512 x 4096 in FP16: 12.2 us by waves of one chunk, 16384 of them
-    const int64_t per_row = ceil_div(channels, 16 / (int64_t)grid.bytes), items = batch * per_row;
+    const int64_t per_row = ceil_div(channels, kStepChannels), items = batch * per_row;
     if (len == 1 && items <= kMaxSize) {
         unsigned row = (unsigned)per_row, all = (unsigned)items;
         void *args[] = {&a, &row, &all};
-        const void *kernel = type == SEQ_FP32 ? (const void *)scan_step<F32> : type == SEQ_FP16 ? (const void *)scan_step<F16>
-                                                                                           : (const void *)scan_step<BF16>;
+        const void *kernel = type == SEQ_FP32 ? step_kernel<F32>(channels) : type == SEQ_FP16 ? step_kernel<F16>(channels) : step_kernel<BF16>(channels);
         return launch(kernel, dim3((unsigned)ceil_div(items, 256)), dim3(256), args, 0, stream);
     }
     void *args[] = {&a};
