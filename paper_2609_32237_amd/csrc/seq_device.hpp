@@ -119,35 +119,36 @@ struct Pack {
     // Keeps the stored form: what was converted from it before is converted
     // again after this, instead of being held in twice the registers.
     __device__ __forceinline__ void hold() { asm volatile("" : "+v"(u)); }
-    // Elements `at` .. of a row of `end`, zeros behind it.  The row's address is
-    // the same in every lane, and an unsigned 32-bit offset of bytes from it needs
-    // no 64-bit address in vector registers.  WHOLE: `end` is a multiple of V.
+    // Elements `at` .. of a row.  The row's address is the same in every lane, and
+    // an unsigned 32-bit offset of bytes from it needs no 64-bit address in vector
+    // registers.
+    __device__ __forceinline__ void load(const T *row, unsigned at) { load((const T *)((const char *)row + at * (unsigned)sizeof(T))); }
+    __device__ __forceinline__ void store(T *row, unsigned at, bool past) const { store((T *)((char *)row + at * (unsigned)sizeof(T)), past); }
+    // The same of a row of `end` elements, zeros behind it.  WHOLE: `end` is a multiple of V.
     template <bool WHOLE>
     __device__ __forceinline__ void load(const T *row, unsigned at, unsigned end) {
-        const char *p = (const char *)row;
         if (WHOLE) {
-            load((const T *)(p + (at < end ? at : end - V) * (unsigned)sizeof(T)));
+            load(row, at < end ? at : end - V);
             u = at < end ? u : U{};
         } else if (at + V <= end) {
-            load((const T *)(p + at * (unsigned)sizeof(T)));
+            load(row, at);
         } else {
             T v[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = at + j < end ? ((const T *)(p + at * (unsigned)sizeof(T)))[j] : (T)0.0f;
+            for (int j = 0; j < V; ++j) v[j] = at + j < end ? row[at + j] : (T)0.0f;
             __builtin_memcpy(&u, v, sizeof(u));
         }
     }
     template <bool WHOLE>
     __device__ __forceinline__ void store(T *row, unsigned at, unsigned end, bool past) const {
-        T *p = (T *)((char *)row + at * (unsigned)sizeof(T));
         if (WHOLE ? at < end : at + V <= end) {
-            store(p, past);
+            store(row, at, past);
         } else if (!WHOLE) {
             T v[V];
             __builtin_memcpy(v, &u, sizeof(u));
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (at + j < end) p[j] = v[j];
+                if (at + j < end) row[at + j] = v[j];
         }
     }
     // the word that holds element j of a 16-bit pack

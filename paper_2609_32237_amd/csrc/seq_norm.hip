@@ -70,19 +70,37 @@ struct Held {
     unsigned lane, end;
 
     __device__ __forceinline__ explicit Held(int channels) : lane(threadIdx.x % THREADS), end(channels) {}
-    // first channel of access n
-    __device__ __forceinline__ unsigned at(int n) const { return (n * THREADS + lane) * V; }
+    // First channel of access n.  Where the width is no multiple of V, the last
+    // access of a row is moved back to its last V channels: the ones that it has in
+    // common with the access before are worked out by both lanes, to the same bits,
+    // and count once in sums (`counts`).  Rows shorter than one access are taken
+    // element by element.
+    __device__ __forceinline__ unsigned own(int n) const { return (n * THREADS + lane) * V; }
+    __device__ __forceinline__ unsigned at(int n) const {
+        const unsigned a = own(n);
+        return WHOLE || a + V <= end || end < V ? a : end - V;
+    }
+    // whether channel j of access n counts in this lane's sums (zeros are loaded where WHOLE)
+    __device__ __forceinline__ bool counts(int n, int j) const { return WHOLE || at(n) + j >= own(n); }
     // a row of an activation; zeros where there is none
     __device__ __forceinline__ void load(P (&p)[N], const void *base, int64_t row, int64_t stride) const {
         const T *r = (const T *)base + row * stride;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             p[n].u = typename P::U{};
-            if (base) p[n].template load<WHOLE>(r, at(n), end);
+            if (!base) continue;
+            if (WHOLE || end < V)
+                p[n].template load<WHOLE>(r, at(n), end);
+            else
+                p[n].load(r, at(n));
         }
     }
     __device__ __forceinline__ void store(const P &p, int n, void *base, int64_t row, int64_t stride, bool past) const {
-        p.template store<WHOLE>((T *)base + row * stride, at(n), end, past);
+        T *r = (T *)base + row * stride;
+        if (WHOLE || end < V)
+            p.template store<WHOLE>(r, at(n), end, past);
+        else if (own(n) < end)
+            p.store(r, at(n), past);
     }
     // a row of weights (times another one) into LDS, four at a time; zeros where there is none
     __device__ __forceinline__ void keep(float *lds, const float *of, const float *times) const {
@@ -92,14 +110,29 @@ struct Held {
             for (int q = 0; q < V / 4; ++q) {
                 Pack<F32, 4> w, s;
                 w.u = Pack<F32, 4>::U{};
-                if (of) w.template load<WHOLE>(of, at(n) + 4 * q, end);
-                if (times) s.template load<WHOLE>(times, at(n) + 4 * q, end);
+                auto four = [&](Pack<F32, 4> &p, const float *row) {
+                    if (WHOLE || end < V)
+                        p.load<WHOLE>(row, at(n) + 4 * q, end);
+                    else
+                        p.load(row, at(n) + 4 * q);
+                };
+                if (of) four(w, of);
+                if (times) four(s, times);
                 float f[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) f[k] = times ? w.get(k) * s.get(k) : w.get(k);
                 w.set(0, f);
                 *(Pack<F32, 4>::U *)(lds + ((n * (V / 4) + q) * THREADS + lane) * 4) = w.u;
             }
+    }
+    // four of this workgroup's sums for the weights' gradients
+    __device__ __forceinline__ void part(float *row, int n, int q, const float (&f)[4]) const {
+        Pack<F32, 4> p;
+        p.set(0, f);
+        if (WHOLE || end < V)
+            p.store<WHOLE>(row, at(n) + 4 * q, end, false);
+        else if (own(n) < end)
+            p.store(row, at(n) + 4 * q, false);
     }
     // weights COUNT i .. COUNT i + COUNT - 1 of access n
     template <int COUNT>
@@ -148,8 +181,9 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_forward(No
 #pragma unroll
             for (int n = 0; n < N; ++n) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) s[0] = fmaf(py[n].get(j), py[n].get(j), s[0]);
-                py[n].hold();
+                for (int j = 0; j < V; ++j) s[0] = at.counts(n, j) ? fmaf(py[n].get(j), py[n].get(j), s[0]) : s[0];
+                // all of the row is here before any of it is written (in place)
+                px[n].hold(), py[n].hold(), pz[n].hold();
             }
             sum(s);
             iy = 1.0f / sqrtf(fmaf(s[0], a.inv_channels, a.eps));
@@ -167,7 +201,7 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_forward(No
                     const int j = 4 * i + k;
                     const float gate = has_z ? pz[n].get(j) * sigmoid(pz[n].get(j)) : 1.0f;
                     f[k] = fmaf(w[k] * gate, py[n].get(j) * iy, px[n].get(j));
-                    s[0] = fmaf(f[k], f[k], s[0]);
+                    s[0] = at.counts(n, j) ? fmaf(f[k], f[k], s[0]) : s[0];
                     o[n][j] = f[k];
                 }
                 p.set(i, f);
@@ -256,9 +290,11 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(N
                     sg[n][j] = sigmoid(pz[n].get(j));
                     float gate, m;
                     const float oh = forward(n, j, w[k], gate, m) * io, p = w[k] * gate * m, v = pn[n].get(j) * pre[k];
-                    s[0] = fmaf(v, oh, s[0]);
-                    s[1] = fmaf(fmaf(io, v, po[n].get(j)), p, s[1]);
-                    s[2] = fmaf(oh, p, s[2]);
+                    if (at.counts(n, j)) {
+                        s[0] = fmaf(v, oh, s[0]);
+                        s[1] = fmaf(fmaf(io, v, po[n].get(j)), p, s[1]);
+                        s[2] = fmaf(oh, p, s[2]);
+                    }
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -309,16 +345,13 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) norm_backward(N
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int i = 0; i < V / 4; ++i) {
-            Pack<F32, 4> p;
             float f[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) f[k] = dw[n][4 * i + k];
-            p.set(0, f);
-            p.template store<WHOLE>(part, at.at(n) + 4 * i, at.end, false);
+            at.part(part, n, i, f);
 #pragma unroll
             for (int k = 0; k < 4; ++k) f[k] = dpre[n][4 * i + k];
-            p.set(0, f);
-            p.template store<WHOLE>(part + a.channels, at.at(n) + 4 * i, at.end, false);
+            at.part(part + a.channels, n, i, f);
         }
 }
 

@@ -123,7 +123,11 @@ template <int V, int W, bool CHAIN>
 struct Tile {
     unsigned chain, tile, b;  // chain, place along it, sequence
     int64_t col;              // first channel
-    int wave, lane, at;       // at: this lane's first channel from col on; lanes beyond the last one repeat it
+    // at: this lane's first channel from col on; lanes beyond the last channels
+    // repeat them.  live: some of its channels are its own; of an odd number of
+    // channels the last lane shares one with its neighbour, in the same wave, and
+    // both write the same bits.
+    int wave, lane, at;
     bool live;
     int64_t t0;               // first token of the wave's chunk
     int count, write;         // its tokens that count, and that exist
@@ -149,8 +153,8 @@ struct Tile {
         col = (int64_t)(chain - b * a.blocks) * (kWave * V);
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
         const int64_t last = a.channels - V - col;
-        live = lane * V <= last;
-        at = live ? lane * V : (int)last;
+        live = lane * V < last + V;
+        at = lane * V <= last ? lane * V : (int)last;
         t0 = ((int64_t)tile * W + wave) * kChunk;
         const int64_t n = valid_tokens(a, b) - t0, l = a.len - t0;
         count = n < 0 ? 0 : n > kChunk ? kChunk : (int)n;
@@ -526,7 +530,8 @@ Cut cut_of(int64_t batch, int64_t len, int64_t channels, int type, bool backward
     // per channel: one leaves registers for two workgroups on a CU, 8 x 4096 x
     // 2048 in 198 us, with two channels 212 us.
     c.lane = 1;
-    if (type != SEQ_FP32 && channels % 2 == 0 && !backward &&
+    if (type != SEQ_FP32 && channels % (2 * kWave) != 1 && !backward &&
+        // (a last channel alone in its block would be shared with another workgroup)
         (c.tiles == 1 || batch * ceil_div(channels, kWave * 2) >= 16))
         c.lane = 2;
     c.blocks = ceil_div(channels, kWave * c.lane);
