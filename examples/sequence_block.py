@@ -1,0 +1,157 @@
+"""A small sequence model from this library's operators, trained and then served.
+
+A time-invariant filter along the tokens is a convolution: ``LongFilter`` takes
+it through the FFT plans, down the columns of (tokens, sequences x channels).
+What the data itself steers is the gated recurrence, between the norms, the gate
+and the scaled residual of each block.
+
+    python examples/sequence_block.py
+
+trains the model on a toy task (each output is a running mean of the input that
+a marker channel starts afresh), then takes a prompt in one call and further
+tokens one at a time, and compares these with the whole sequence at once.
+"""
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+from paper_2609_32237_amd import seq_api as sq  # noqa: E402
+from paper_2609_32237_amd import torch_api as mf  # noqa: E402
+
+EPS = 1e-5
+
+
+class LongFilter:
+    """y_t = sum over j of taps_j x_(t-j), each channel with its own taps, for up
+    to ``tokens`` tokens: one forward and one inverse FFT of twice the length."""
+
+    def __init__(self, taps: torch.Tensor, tokens: int, batch: int):
+        self.taps, self.batch = taps, batch
+        self.n = max(1024, 1 << (tokens + len(taps) - 1).bit_length())
+        if self.n > 16384:
+            raise ValueError("columns of up to 16384 points")
+        columns = batch * taps.shape[1]
+        self.there = mf.Plan(self.n, columns, columns, 1)
+        self.back = mf.Plan(self.n, columns, columns, 1, direction=mf.FFT_INVERSE)
+        self.spectrum = self._transform(self.there, taps[:, None].expand(-1, batch, -1)) / self.n
+
+    def _transform(self, plan, x):
+        z = torch.zeros(self.n, x.shape[1] * x.shape[2], dtype=torch.complex64, device=x.device)
+        z[:x.shape[0]] = x.reshape(x.shape[0], -1)
+        return plan.execute(z, torch.empty_like(z))
+
+    def __call__(self, x):
+        """(batch, tokens, channels)"""
+        z = self._transform(self.there, x.transpose(0, 1)) * self.spectrum
+        y = self.back.execute(z, torch.empty_like(z))[:x.shape[1]].real
+        return y.reshape(x.shape[1], self.batch, -1).transpose(0, 1).contiguous()
+
+    def step(self, past):
+        """The last token of ``past`` (batch, tokens so far, channels)."""
+        k = min(past.shape[1], len(self.taps))
+        return (past[:, past.shape[1] - k:].flip(1) * self.taps[:k]).sum(1)
+
+
+def make_weights(inputs, width, blocks, seed=0, device="cuda"):
+    gen = torch.Generator(device=device).manual_seed(seed)
+
+    def dense(rows, cols):
+        return torch.empty(rows, cols, device=device).normal_(0.0, rows**-0.5, generator=gen)
+
+    w = dict(embed=dense(inputs, width), pre=torch.ones(width, device=device), head=dense(width, 1) * 0.1, blocks=[])
+    for _ in range(blocks):
+        w["blocks"].append(dict(inner=dense(width, 4 * width), outer=dense(width, width),
+                                rate=torch.exp(torch.empty(width, device=device).uniform_(-4.0, 0.0, generator=gen)),
+                                post=torch.ones(width, device=device), scale=torch.full((width,), 0.5, device=device),
+                                pre=torch.ones(width, device=device)))
+    return w
+
+
+def leaves(w):
+    return [v for k, v in w.items() if k != "blocks"] + [v for b in w["blocks"] for v in b.values()]
+
+
+def _project(h, weight):
+    return (h.reshape(-1, h.shape[-1]) @ weight).view(*h.shape[:-1], -1)
+
+
+def forward(w, u, lengths=None, train=False):
+    """(batch, tokens, inputs) -> (batch, tokens), and the state of each block."""
+    scan = sq.gated_scan_train if train else sq.gated_scan
+    norm = sq.residual_norm_train if train else sq.residual_norm
+    states = []
+    x, h = norm(_project(u, w["embed"]), pre=w["pre"], eps=EPS)
+    for b in w["blocks"]:
+        v, r, g, z = _project(h, b["inner"]).chunk(4, -1)
+        y, state = scan(v, r, g, b["rate"], None, lengths)
+        states.append(state)
+        x, h = norm(x, _project(y, b["outer"]), z.contiguous(), b["post"], b["scale"], b["pre"], eps=EPS)
+    return _project(h, w["head"])[..., 0], states
+
+
+def step(w, u, states):
+    """One token (batch, inputs) after those that the states have seen; the states are updated in place."""
+    x, h = sq.residual_norm(u @ w["embed"], pre=w["pre"], eps=EPS)
+    for b, state in zip(w["blocks"], states):
+        v, r, g, z = (h @ b["inner"]).chunk(4, -1)
+        y = sq.gated_scan_step(v, r, g, b["rate"], state)
+        x, h = sq.residual_norm(x, y @ b["outer"], z, b["post"], b["scale"], b["pre"], eps=EPS)
+    return (h @ w["head"])[:, 0]
+
+
+def toy(batch, tokens, gen):
+    """Noise, now and then a marker; the target is the mean of the noise since the last marker."""
+    noise = torch.empty(batch, tokens, device="cuda").normal_(generator=gen)
+    marker = (torch.rand(batch, tokens, device="cuda", generator=gen) < 0.05).float()
+    marker[:, 0] = 1
+    total = torch.cumsum(noise, 1)
+    starts = torch.where(marker.bool(), torch.arange(tokens, device="cuda"), 0).cummax(1).values
+    count = torch.arange(tokens, device="cuda") - starts + 1
+    mean = (total - torch.where(starts > 0, total.gather(1, (starts - 1).clamp_min(0)), 0.0)) / count
+    return torch.stack([noise, marker], -1), mean
+
+
+def train(steps=60, batch=16, tokens=300, width=64, blocks=2, seed=0):
+    """Adam on the toy task; returns the weights and the losses."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    # the long filter gives the model smoothed copies of the input beside the input itself
+    decays = torch.tensor([0.5, 0.8, 0.95], device="cuda")
+    taps = (1 - decays) * decays ** torch.arange(128, device="cuda")[:, None]
+    smooth = LongFilter(taps, tokens, batch)
+    w = make_weights(2 + 3, width, blocks, seed)
+    for v in leaves(w):
+        v.requires_grad_(True)
+    opt, losses = torch.optim.Adam(leaves(w), lr=1e-2), []
+    for _ in range(steps):
+        u, target = toy(batch, tokens, gen)
+        u = torch.cat([u, smooth(u[..., :1].expand(-1, -1, 3))], -1)
+        out, _ = forward(w, u, train=True)
+        loss = (out - target).square().mean()
+        opt.zero_grad()
+        loss.backward()
+        opt.step()
+        losses.append(loss.item())
+    for v in leaves(w):
+        v.requires_grad_(False)
+    return w, smooth, losses
+
+
+def serve(w, smooth, prompt=200, more=40, seed=1):
+    """A prompt at once, then token by token; the largest difference from the whole sequence at once."""
+    u, _ = toy(smooth.batch, prompt + more, torch.Generator(device="cuda").manual_seed(seed))
+    raw = u[..., :1].expand(-1, -1, 3)
+    whole, _ = forward(w, torch.cat([u, smooth(raw)], -1))
+    out, states = forward(w, torch.cat([u, smooth(raw)], -1)[:, :prompt])
+    got = [out]
+    for t in range(prompt, prompt + more):
+        got.append(step(w, torch.cat([u[:, t], smooth.step(raw[:, :t + 1])], -1), states)[:, None])
+    return (torch.cat(got, 1) - whole).abs().max().item()
+
+
+if __name__ == "__main__":
+    weights, long_filter, history = train()
+    print("loss: first %.4f, last %.4f" % (history[0], sum(history[-5:]) / 5))
+    print("token by token and at once differ by at most %.2e" % serve(weights, long_filter))

@@ -55,9 +55,11 @@ __device__ __forceinline__ int64_t valid_tokens(const ScanArgs &a, unsigned b) {
 // (512 workgroups at one counter queued for 8 us), the earlier tiles of every
 // chain first: a tile waits only for tiles that started before it, and the
 // first waits for none, so every wait ends.
-// kWindow: with 8, the words took registers that keep two workgroups on a CU
-// (8 x 4096 x 2048 forward 135 us, with 4 123 us).
-constexpr int kWindow = 4;
+// kWindow: with two channels to a lane, the words of 8 tiles take registers that
+// keep two workgroups on a CU (8 x 4096 x 2048 forward 135 us, with 4 123 us);
+// with one, 8 are faster where the chains are few (1 x 65536 x 1024 148 and 143 us).
+template <int V>
+constexpr int kWindow = V == 1 ? 8 : 4;
 constexpr unsigned kGroups = 4, kCounterPitch = 32;
 constexpr uint32_t kEmpty = 0xffffffffu, kState = 0xfffffffeu;  // in place of A: NaNs that no published A has
 // A word that never arrives (a workspace that another call writes) must not
@@ -80,11 +82,12 @@ __device__ __forceinline__ uint64_t peek(const uint64_t *p) {
 // (this lane's first channel; `pitch` words from tile to tile).
 template <int V>
 __device__ __forceinline__ void look_back(const uint64_t *words, int64_t pitch, int64_t before, float (&h)[V]) {
+    constexpr int kMost = kWindow<V>;
     for (int poll = 0; poll < kMaxPolls; ++poll) {
-        const int window = poll == 0 ? 1 : kWindow;
-        uint64_t w[kWindow][V];
+        const int window = poll == 0 ? 1 : kMost;
+        uint64_t w[kMost][V];
 #pragma unroll
-        for (int i = 0; i < kWindow; ++i)
+        for (int i = 0; i < kMost; ++i)
             if (i < window && i < before)
 #pragma unroll
                 for (int j = 0; j < V; ++j) w[i][j] = peek(words + (before - 1 - i) * pitch + j);
@@ -92,7 +95,7 @@ __device__ __forceinline__ void look_back(const uint64_t *words, int64_t pitch, 
 #pragma unroll
         for (int j = 0; j < V; ++j) have[j] = false;
 #pragma unroll
-        for (int i = kWindow - 1; i >= 0; --i)
+        for (int i = kMost - 1; i >= 0; --i)
             if (i < window && i < before)
 #pragma unroll
                 for (int j = 0; j < V; ++j) {

@@ -1,0 +1,42 @@
+"""The example model: its long filter against the direct sum, training that
+learns, and token-by-token serving that gives what the whole sequence gives."""
+import importlib.util
+import os
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def ex():
+    spec = importlib.util.spec_from_file_location("sequence_block", os.path.join(ROOT, "examples", "sequence_block.py"))
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    return mod
+
+
+def test_long_filter(ex):
+    gen = torch.Generator().manual_seed(0)
+    taps, x = torch.randn(50, 3, generator=gen), torch.randn(4, 700, 3, generator=gen)
+    f = ex.LongFilter(taps.cuda(), 700, 4)
+    want = torch.zeros(4, 700, 3, dtype=torch.float64)
+    for j in range(50):
+        want[:, j:] += taps[j].double() * x[:, :700 - j].double()
+    got = f(x.cuda()).cpu().double()
+    # FP32 transforms of 1024 points: relative L2 error below 1e-6 each way
+    assert (got - want).norm() / want.norm() < 1e-5
+    for t in (0, 10, 49, 50, 699):
+        assert torch.allclose(f.step(x[:, :t + 1].cuda()).cpu().double(), want[:, t], rtol=1e-4, atol=1e-4)
+
+
+def test_train_and_serve(ex):
+    w, smooth, losses = ex.train()
+    assert all(torch.isfinite(v).all() for v in ex.leaves(w))
+    assert sum(losses[-5:]) / 5 < 0.5 * losses[0]
+    # FP32 with another order of sums in the products of one token and of many: about 1e-6 of the
+    # activations, amplified by the norms of two blocks
+    assert ex.serve(w, smooth) < 1e-3

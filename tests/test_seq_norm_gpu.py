@@ -182,6 +182,42 @@ def test_in_place(sq, dtype, d):
         assert all(torch.equal(a, b) for a, b in zip(got, grads))
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("rows, d", [(3, 5), (300, 99), (2100, 515), (300, 1001), (600, 2055), (40, 4099), (20, 8191), (9, 16383)])
+def test_in_place_with_odd_widths(sq, dtype, rows, d):
+    """Accesses that share channels with their neighbours read all of them before either writes; rows in a row."""
+    (x, y, z, go, gn), w = inputs(rows, d, dtype, 14)
+    stats = sq.residual_norm_stats(x)
+    want = sq.residual_norm(x, y, z, *w, eps=EPS, stats=stats)
+    grads = sq.residual_norm_backward(go, gn, x, y, z, *w, stats, eps=EPS)
+    wo, wn = ref.norm(*(v.cpu().double() for v in (x, y, z, *w)), EPS)
+    ref.check(want[0], wo, "out")
+    ref.check(want[1], wn, "normed")
+    v = [t.clone() for t in (x, y, z)]
+    sq.residual_norm(*v, *w, eps=EPS, out=v[0], normed=v[1])
+    assert torch.equal(v[0], want[0]) and torch.equal(v[1], want[1])
+    v = [t.clone() for t in (go, gn, x, y, z)]
+    got = sq.residual_norm_backward(*v, *w, stats, eps=EPS, out=(v[0], v[1], v[4]))
+    assert all(torch.equal(a, b) for a, b in zip(got, grads))
+
+
+@pytest.mark.parametrize("d", [3, 100, 515, 1024, 20000])
+def test_writes_nothing_outside(sq, d):
+    """Outputs inside wider buffers: what surrounds them keeps its values."""
+    for dtype in TYPES:
+        (x, y, z, go, gn), w = inputs(11, d, dtype, 15)
+        wide = [torch.full((13, d + 6), 7.0, dtype=dtype, device="cuda") for _ in range(5)]
+        inner = [v[1:-1, 3:-3] for v in wide]
+        stats = sq.residual_norm_stats(x)
+        sq.residual_norm(x, y, z, *w, eps=EPS, out=inner[0], normed=inner[1], stats=stats)
+        sq.residual_norm_backward(go, gn, x, y, z, *w, stats, eps=EPS, out=inner[2:])
+        want = [*sq.residual_norm(x, y, z, *w, eps=EPS), *sq.residual_norm_backward(go, gn, x, y, z, *w, stats, eps=EPS)[:3]]
+        for v, part, expect in zip(wide, inner, want):
+            assert torch.equal(part, expect)
+            part.fill_(7.0)
+            assert (v == 7.0).all()
+
+
 @pytest.mark.parametrize("rows, d", [(3000, 1024), (40, 16384), (20000, 64)])
 def test_same_bits_again_and_on_other_streams(sq, rows, d):
     (x, y, z, go, gn), w = inputs(rows, d, torch.bfloat16, 9)

@@ -2,6 +2,8 @@
 long, odd widths, strides, lengths that leave a sequence empty, in place, other
 streams, graphs, extreme gates; its gradient against the formula's and against
 differences."""
+import itertools
+
 import pytest
 import torch
 
@@ -198,6 +200,43 @@ def test_in_place(sq, dtype, t):
     wide = torch.empty(2, t, 300, dtype=dtype, device="cuda")
     got = sq.gated_scan_backward(dy, x, r, g, rate, saved, grad_state=dlast, out=wide.split(100, -1))
     assert torch.equal(wide, torch.cat(grads[:3], -1))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("b, t, d", [(2, 1, 129), (3, 1, 1001), (2, 40, 131), (1, 300, 129), (2, 700, 255), (20, 300, 131)])
+def test_in_place_with_odd_widths(sq, dtype, b, t, d):
+    """Lanes that share a channel with their neighbour read all of it before either writes."""
+    x, r, g, dy, rate, state, dlast = inputs(b, t, d, dtype, 16)
+    y, last = sq.gated_scan(x, r, g, rate, state)
+    wy, wlast = ref.scan(*(v.cpu().double() for v in (x, r, g, rate, state)))
+    ref.check(y, wy, "y")
+    ref.check(last, wlast, "state")
+    for k in range(3):
+        v = [w.clone() for w in (x, r, g)]
+        h = state.clone()
+        sq.gated_scan(*v, rate, h, out=v[k], state_out=h)
+        assert torch.equal(v[k], y) and torch.equal(h, last)
+
+
+@pytest.mark.parametrize("d", [4, 70])
+def test_writes_nothing_outside(sq, d):
+    """Outputs inside wider buffers: what surrounds them keeps its values."""
+    for dtype, t in itertools.product(TYPES, (1, 20, 300)):
+        for pad in (1, 3):
+            x, r, g, dy, rate, state, dlast = inputs(2, t, d + pad, dtype, 17)
+            x, r, g, dy = (v[..., :d] for v in (x, r, g, dy))
+            rate, state, dlast = rate[:d].contiguous(), state[:, :d].contiguous(), dlast[:, :d].contiguous()
+            wide = [torch.full((2, t + 2, d + 2 * pad), 7.0, dtype=dtype, device="cuda") for _ in range(4)]
+            y, dx, dr, dg = (w[:, 1:-1, pad:-pad] for w in wide)
+            saved = sq.gated_scan_saved(x)
+            sq.gated_scan(x, r, g, rate, state, out=y, saved=saved)
+            sq.gated_scan_backward(dy, x, r, g, rate, saved, grad_state=dlast, out=(dx, dr, dg))
+            want = sq.gated_scan(x, r, g, rate, state)[0]
+            grads = sq.gated_scan_backward(dy, x, r, g, rate, saved, grad_state=dlast)[:3]
+            for w, inner, expect in zip(wide, (y, dx, dr, dg), (want, *grads)):
+                assert torch.equal(inner, expect)
+                inner.fill_(7.0)
+                assert (w == 7.0).all()
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
