@@ -5,7 +5,8 @@ before and after a block with its gate and scaled residual.
 Activations are float32, float16 or bfloat16 tensors whose last axis is
 consecutive in memory (the other axes may be strided: slices of a wider
 projection need no copy); weights, states and statistics are contiguous
-float32.  Every function runs on the current stream, or on ``stream``.
+float32.  Every function runs on the current stream, or with ``stream=`` (a
+torch stream or a handle) on that one, where its new tensors then belong.
 ``gated_scan_train`` and ``residual_norm_train`` are the same operators as
 autograd functions.
 """
@@ -80,17 +81,31 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _workspace(nbytes: int, given, like: torch.Tensor, stream):
+def _workspace(nbytes: int, given, like: torch.Tensor):
     """(tensor, pointer) of scratch memory: the caller's, or new memory of the current stream."""
     if nbytes == 0:
         return None, None
     if given is None:
         given = _new((nbytes,), (1,), dtype=torch.uint8, device=like.device)
-        if stream is not None:  # it is given back to the current stream's pool while `stream` may still use it
-            given.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
     elif given.device != like.device or not given.is_contiguous() or given.numel() * given.element_size() < nbytes:
         raise ValueError(f"workspace must be contiguous, of at least {nbytes} bytes, on the device of the activations")
     return given, given.data_ptr()
+
+
+def _on_its_stream(call):
+    """``stream=``: the call as if that stream were the current one, so that new
+    memory comes from its pool too (the current stream's may still be in use there)."""
+
+    @functools.wraps(call)
+    def on_stream(*args, stream=None, **kwargs):
+        if stream is None:
+            return call(*args, **kwargs)
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream))
+        with torch.cuda.stream(stream):
+            return call(*args, **kwargs)
+
+    return on_stream
 
 
 def gated_scan_saved(x: torch.Tensor) -> torch.Tensor:
@@ -100,8 +115,8 @@ def gated_scan_saved(x: torch.Tensor) -> torch.Tensor:
     return _new((b, n, d), (n * d, d, 1), dtype=_fp32, device=x.device)
 
 
-def gated_scan(x, r, g, rate, state=None, lengths=None, *, out=None, state_out=None, saved=None, workspace=None,
-               stream=None):
+@_on_its_stream
+def gated_scan(x, r, g, rate, state=None, lengths=None, *, out=None, state_out=None, saved=None, workspace=None):
     """The gated linear recurrence of each channel of (batch, tokens, channels):
 
         h_t = h_(t-1) + q_t (c_t - h_(t-1)),  q_t = rate sigmoid(r_t),  c_t = sigmoid(g_t) x_t
@@ -125,25 +140,27 @@ def gated_scan(x, r, g, rate, state=None, lengths=None, *, out=None, state_out=N
         last = state_out.data_ptr()
     else:
         last = _weight(state_out, "state_out", states, x)
-    _, ws = _workspace(_scan_workspace_bytes(b, t, d, kind, 0), workspace, x, stream)
+    _, ws = _workspace(_scan_workspace_bytes(b, t, d, kind, 0), workspace, x)
     _l.check(_l.lib.seq_scan_forward(
         b, t, d, kind, x.data_ptr(), r.data_ptr(), g.data_ptr(), strides, _weight(rate, "rate", (d,), x),
         _weight(state, "state", states, x), _weight(lengths, "lengths", (b,), x, torch.int32), out.data_ptr(), last,
-        _weight(saved, "saved", (b, -(-t // SEQ_SCAN_CHUNK), d), x), ws, _stream(stream)), "seq_scan_forward")
+        _weight(saved, "saved", (b, -(-t // SEQ_SCAN_CHUNK), d), x), ws, _stream(None)), "seq_scan_forward")
     return out, state_out
 
 
-def gated_scan_step(x, r, g, rate, state, *, out=None, stream=None):
+@_on_its_stream
+def gated_scan_step(x, r, g, rate, state, *, out=None):
     """One token (batch, channels) of ``gated_scan``; ``state`` is updated in place.  Returns y."""
     if x.dim() != 2 or r.dim() != 2 or g.dim() != 2:
         raise ValueError("x, r and g must have 2 axes")
     y, _ = gated_scan(x.unsqueeze(1), r.unsqueeze(1), g.unsqueeze(1), rate, state,
-                      out=None if out is None else out.unsqueeze(1), state_out=state, stream=stream)
+                      out=None if out is None else out.unsqueeze(1), state_out=state)
     return y.squeeze(1) if out is None else out
 
 
+@_on_its_stream
 def gated_scan_backward(grad_out, x, r, g, rate, saved, lengths=None, *, grad_state=None, out=(None, None, None),
-                        workspace=None, stream=None):
+                        workspace=None):
     """Gradient of ``gated_scan``: (dx, dr, dg, drate, dstate) from the
     gradients of y and of the state after the last token (None: zeros).
     ``out``: tensors for dx, dr and dg, slices of one buffer for example."""
@@ -155,13 +172,13 @@ def gated_scan_backward(grad_out, x, r, g, rate, saved, lengths=None, *, grad_st
         raise TypeError("rate or saved is missing")
     drate = _new((d,), (1,), dtype=_fp32, device=x.device)
     dstate = _new((b, d), (d, 1), dtype=_fp32, device=x.device)
-    _, ws = _workspace(_scan_workspace_bytes(b, t, d, kind, 1), workspace, x, stream)
+    _, ws = _workspace(_scan_workspace_bytes(b, t, d, kind, 1), workspace, x)
     _l.check(_l.lib.seq_scan_backward(
         b, t, d, kind, grad_out.data_ptr(), x.data_ptr(), r.data_ptr(), g.data_ptr(),
         strides, _weight(rate, "rate", (d,), x),
         _weight(saved, "saved", (b, -(-t // SEQ_SCAN_CHUNK), d), x), _weight(lengths, "lengths", (b,), x, torch.int32),
         _weight(grad_state, "grad_state", (b, d), x), dx.data_ptr(), dr.data_ptr(), dg.data_ptr(), drate.data_ptr(),
-        dstate.data_ptr(), ws, _stream(stream)), "seq_scan_backward")
+        dstate.data_ptr(), ws, _stream(None)), "seq_scan_backward")
     return dx, dr, dg, drate, dstate
 
 
@@ -172,8 +189,8 @@ def residual_norm_stats(x: torch.Tensor) -> torch.Tensor:
     return torch.empty((*x.shape[:-1], 2), dtype=_fp32, device=x.device)
 
 
-def residual_norm(x, y=None, z=None, post=None, scale=None, pre=None, *, eps: float, out=None, normed=None, stats=None,
-                  stream=None):
+@_on_its_stream
+def residual_norm(x, y=None, z=None, post=None, scale=None, pre=None, *, eps: float, out=None, normed=None, stats=None):
     """The end of a block and the beginning of the next one, over the last axis:
 
         o = x + scale post (y / rms(y)) silu(z),  n = pre o / rms(o)
@@ -186,7 +203,7 @@ def residual_norm(x, y=None, z=None, post=None, scale=None, pre=None, *, eps: fl
     if x.dim() != 2:  # as rows, without a copy
         shape, part = x.shape, [v if v is None else v.view(-1, v.shape[-1]) for v in (x, y, z, out, normed)]
         o2, n2 = residual_norm(*part[:3], post, scale, pre, eps=eps, out=part[3], normed=part[4],
-                               stats=None if stats is None else stats.view(-1, 2), stream=stream)
+                               stats=None if stats is None else stats.view(-1, 2))
         return (x if y is None else o2.view(shape) if out is None else out,
                 None if pre is None else n2.view(shape) if normed is None else normed)
     kind = _type_of(x, "x", 2)
@@ -199,19 +216,19 @@ def residual_norm(x, y=None, z=None, post=None, scale=None, pre=None, *, eps: fl
     _l.check(_l.lib.seq_norm_forward(
         rows, d, kind, x.data_ptr(), _ptr(y), _ptr(z), strides, _weight(post, "post", (d,), x),
         _weight(scale, "scale", (d,), x), _weight(pre, "pre", (d,), x), eps, _ptr(out), _ptr(normed),
-        _weight(stats, "stats", (rows, 2), x), _stream(stream)), "seq_norm_forward")
+        _weight(stats, "stats", (rows, 2), x), _stream(None)), "seq_norm_forward")
     return x if y is None else out, normed
 
 
+@_on_its_stream
 def residual_norm_backward(grad_out, grad_normed, x, y, z, post, scale, pre, stats, *, eps: float,
-                           out=(None, None, None), workspace=None, stream=None):
+                           out=(None, None, None), workspace=None):
     """Gradient of ``residual_norm``: (dx, dy, dz, dpost, dscale, dpre), None
     where the argument is.  ``grad_out`` may be None (zeros), ``grad_normed``
     is None where ``pre`` is.  ``out``: tensors for dx, dy and dz."""
     if x.dim() != 2:
         shape, part = x.shape, [v if v is None else v.view(-1, v.shape[-1]) for v in (grad_out, grad_normed, x, y, z, *out)]
-        found = residual_norm_backward(*part[:5], post, scale, pre, stats.view(-1, 2), eps=eps, out=part[5:], workspace=workspace,
-                                       stream=stream)
+        found = residual_norm_backward(*part[:5], post, scale, pre, stats.view(-1, 2), eps=eps, out=part[5:], workspace=workspace)
         return tuple(v if v is None else v.view(shape) if given is None else given for v, given in zip(found, out)) + found[3:]
     kind = _type_of(x, "x", 2)
     rows, d = x.shape
@@ -222,12 +239,12 @@ def residual_norm_backward(grad_out, grad_normed, x, y, z, post, scale, pre, sta
     if stats is None:
         raise TypeError("stats is missing")
     grads = [None if w is None else _new((d,), (1,), dtype=_fp32, device=x.device) for w in (post, scale, pre)]
-    _, ws = _workspace(_norm_workspace_bytes(rows, d, kind), workspace, x, stream)
+    _, ws = _workspace(_norm_workspace_bytes(rows, d, kind), workspace, x)
     _l.check(_l.lib.seq_norm_backward(
         rows, d, kind, _ptr(grad_out), _ptr(grad_normed), x.data_ptr(), _ptr(y), _ptr(z), strides,
         _weight(post, "post", (d,), x), _weight(scale, "scale", (d,), x), _weight(pre, "pre", (d,), x), eps,
         _weight(stats, "stats", (rows, 2), x), dx.data_ptr(), _ptr(dy), _ptr(dz), *map(_ptr, grads), ws,
-        _stream(stream)), "seq_norm_backward")
+        _stream(None)), "seq_norm_backward")
     return (dx, dy, dz, *grads)
 
 

@@ -287,6 +287,29 @@ def test_other_streams_at_once(sq):
     assert torch.equal(out, want[0][0]) and torch.equal(last, want[0][1])
 
 
+def test_stream_argument_and_new_memory(sq):
+    """New tensors of a call on another stream belong to that stream: memory that the
+    current stream has given back but still reads is not handed to it."""
+    x, r, g, dy, rate, state, dlast = inputs(1, 2000, 256, torch.float16, 18)
+    saved = sq.gated_scan_saved(x)
+    want = sq.gated_scan(x, r, g, rate, state, saved=saved)
+    grads = sq.gated_scan_backward(dy, x, r, g, rate, saved, grad_state=dlast)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (side, side.cuda_stream):
+        for _ in range(3):
+            busy = torch.full_like(x, 3.0)
+            total = torch.zeros_like(x)
+            for _ in range(20):
+                total += busy
+            del busy  # its memory is free for the current stream's next tensor while `total` is still summed up
+            got = sq.gated_scan(x, r, g, rate, state, stream=stream)
+            back = sq.gated_scan_backward(dy, x, r, g, rate, saved, grad_state=dlast, stream=stream)
+            torch.cuda.synchronize()
+            assert (total == 60.0).all()
+            assert all(torch.equal(a, b) for a, b in zip((*got, *back), (*want, *grads)))
+
+
 @pytest.mark.parametrize("b, t, d", [(1, 2500, 128), (4, 100, 256), (4, 1, 256)])
 def test_graph_replays(sq, b, t, d):
     x, r, g, dy, rate, state, dlast = inputs(b, t, d, torch.bfloat16, 11)
