@@ -80,7 +80,8 @@ enum { SEQ_SCAN_CHUNK = 16 };
  *   state_out    (batch, channels) FP32 or NULL: the state after the last
  *                token that counts; may be `state` itself.
  *   saved        NULL, or seq_scan_saved_bytes() for the gradient: the state
- *                before every 16th token, (batch, ceil(len / 16), channels).
+ *                before every 16th token that counts, (batch, ceil(len / 16),
+ *                channels).
  *   workspace    seq_scan_workspace_bytes(.., 0) bytes, aligned to 16; may be
  *                NULL where that is 0.
  * Returns SEQ_OK, SEQ_EINVAL, SEQ_EUNSUPPORTED, SEQ_EALIGN or SEQ_EHIP.

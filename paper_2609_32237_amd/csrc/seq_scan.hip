@@ -132,8 +132,9 @@ struct Tile {
     // both write the same bits.
     int wave, lane, at;
     bool live;
-    int64_t t0;               // first token of the wave's chunk
-    int count, write;         // its tokens that count, and that exist
+    int64_t n, t0;            // tokens of the sequence that count; first token of the wave's chunk
+    int count, write;         // the chunk's tokens that count, and that exist
+    unsigned tiles;           // of the chain: those behind the last token that counts only write zeros
 
     // False where this workgroup is left over (its group has fewer chains than others).
     template <bool BACK>
@@ -148,7 +149,7 @@ struct Tile {
             const unsigned n = __builtin_amdgcn_readfirstlane(ticket);
             tile = n / chains, chain = first + (n - tile * chains);
             if (tile >= a.tiles) return false;
-            if (BACK) tile = a.tiles - 1 - tile;
+            if (BACK) tile = a.tiles - 1 - tile;  // the last tile first
         } else {
             tile = 0, chain = blockIdx.x;
         }
@@ -159,10 +160,21 @@ struct Tile {
         live = lane * V < last + V;
         at = lane * V <= last ? lane * V : (int)last;
         t0 = ((int64_t)tile * W + wave) * kChunk;
-        const int64_t n = valid_tokens(a, b) - t0, l = a.len - t0;
-        count = n < 0 ? 0 : n > kChunk ? kChunk : (int)n;
+        n = valid_tokens(a, b);
+        tiles = n > W * kChunk ? (unsigned)((n + W * kChunk - 1) / (W * kChunk)) : 1;
+        const int64_t c = n - t0, l = a.len - t0;
+        count = c < 0 ? 0 : c > kChunk ? kChunk : (int)c;
         write = l < 0 ? 0 : l > kChunk ? kChunk : (int)l;
         return true;
+    }
+    __device__ __forceinline__ bool idle() const { return CHAIN && tile >= tiles; }
+    template <typename E>
+    __device__ __forceinline__ void zeros(void *out, int64_t stride_b, int64_t stride_t, bool past) const {
+        typename E::T *p = (typename E::T *)out + b * stride_b + t0 * stride_t + col;
+        Pack<E, V> none;
+        none.u = typename Pack<E, V>::U{};
+        if (live)
+            for (int s = 0; s < write; ++s) none.store(p + s * stride_t + at, past);
     }
     __device__ __forceinline__ uint64_t *words(const ScanArgs &a) const {
         return a.words + (int64_t)chain * a.tiles * (kWave * V) + lane * V;
@@ -216,6 +228,10 @@ __global__ void __launch_bounds__(kWave *W) scan_forward(ScanArgs a) {
     __shared__ float carry[kWave * V];
     Tile<V, W, CHAIN> k;
     if (!k.template find<false>(a)) return;
+    if (k.idle()) {
+        k.template zeros<E>(a.y, a.yb, a.yt, a.stream_out);
+        return;
+    }
     const T *x = (const T *)a.x + k.b * a.xb + k.t0 * a.xt + k.col, *r = (const T *)a.r + k.b * a.rb + k.t0 * a.rt + k.col;
     const T *g = (const T *)a.g + k.b * a.gb + k.t0 * a.gt + k.col;
     const int64_t d = k.col + k.at;
@@ -257,7 +273,7 @@ __global__ void __launch_bounds__(kWave *W) scan_forward(ScanArgs a) {
     if (k.wave == 0) {
         float tA[V], tH[V];
         uint64_t *words = k.words(a);
-        if (CHAIN && k.tile + 1 < a.tiles) {
+        if (CHAIN && k.tile + 1 < k.tiles) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 tA[j] = A[j], tH[j] = H[j];
@@ -275,7 +291,7 @@ __global__ void __launch_bounds__(kWave *W) scan_forward(ScanArgs a) {
         } else {
             look_back<V>(words, kWave * V, k.tile, h);
         }
-        if (CHAIN && k.tile + 1 < a.tiles) {
+        if (CHAIN && k.tile + 1 < k.tiles) {
 #pragma unroll
             for (int j = 0; j < V; ++j) publish(words + (int64_t)k.tile * (kWave * V) + j, state_word(fmaf(tA[j], h[j], tH[j])));
         }
@@ -295,7 +311,7 @@ __global__ void __launch_bounds__(kWave *W) scan_forward(ScanArgs a) {
             }
         }
     }
-    if (a.saved && k.write && k.live) {
+    if (a.saved && (k.count || k.t0 == 0) && k.write && k.live) {
         const int64_t chunk = k.t0 / kChunk;
 #pragma unroll
         for (int j = 0; j < V; ++j) a.saved[(k.b * a.chunks + chunk) * a.channels + d + j] = h[j];
@@ -320,8 +336,8 @@ __global__ void __launch_bounds__(kWave *W) scan_forward(ScanArgs a) {
         states(std::true_type{});
     else
         states(std::false_type{});
-    // the wave with the last token, or the first one where there is none
-    if (a.state_out && k.live && (k.write ? k.t0 + k.write == a.len : a.len == 0 && k.wave == 0)) {
+    // the wave with the last token that counts, or the first one where there is none
+    if (a.state_out && k.live && (k.n ? k.t0 < k.n && k.n <= k.t0 + kChunk : k.t0 == 0)) {
 #pragma unroll
         for (int j = 0; j < V; ++j) a.state_out[k.b * a.channels + d + j] = h[j];
     }
@@ -338,6 +354,16 @@ __global__ void __launch_bounds__(kWave *W) scan_backward(ScanArgs a) {
     __shared__ float carry[kWave * V];
     Tile<V, W, CHAIN> k;
     if (!k.template find<true>(a)) return;
+    if (k.idle()) {
+        k.template zeros<E>(a.dx, a.dxb, a.dxt, a.stream_out);
+        k.template zeros<E>(a.dr, a.drb, a.drt, a.stream_out);
+        k.template zeros<E>(a.dg, a.dgb, a.dgt, a.stream_out);
+        if (k.wave == 0 && k.live) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) a.partial[((int64_t)k.tile * a.batch + k.b) * a.channels + k.col + k.at + j] = 0.0f;
+        }
+        return;
+    }
     const T *x = (const T *)a.x + k.b * a.xb + k.t0 * a.xt + k.col, *r = (const T *)a.r + k.b * a.rb + k.t0 * a.rt + k.col;
     const T *g = (const T *)a.g + k.b * a.gb + k.t0 * a.gt + k.col, *dy = (const T *)a.dy + k.b * a.dyb + k.t0 * a.dyt + k.col;
     const int64_t d = k.col + k.at, chunk = k.t0 / kChunk;
@@ -396,7 +422,7 @@ __global__ void __launch_bounds__(kWave *W) scan_backward(ScanArgs a) {
     if (k.wave == W - 1) {
         float tA[V], tK[V];
         uint64_t *words = k.words(a);
-        const unsigned place = a.tiles - 1 - k.tile;  // along the chain
+        const unsigned place = k.tiles - 1 - k.tile;  // along the chain
         if (CHAIN && k.tile > 0) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
