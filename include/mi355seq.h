@@ -139,7 +139,7 @@ size_t seq_scan_workspace_bytes(int64_t batch, int64_t len, int64_t channels, in
  *                contiguous.
  *   post, scale, pre  (channels) FP32.  scale NULL: 1.  pre NULL: no second
  *                norm, then normed is NULL too.
- *   eps          > 0.
+ *   eps          a normal number > 0 (at least 1.2e-38).
  *   out          o; may be x itself with the same stride.
  *   normed       n, from o before it is rounded; may be y or z itself with the
  *                same stride.

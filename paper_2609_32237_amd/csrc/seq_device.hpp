@@ -60,7 +60,8 @@ __device__ __forceinline__ float sigmoid(float v) {
 
 // Sum over groups of WIDTH (4, 8 or 16) lanes that follow each other, in every
 // lane, by moves between the lanes of 16; for 4 and 8 the 16 lanes hold the
-// same groups.
+// same groups.  The order of the sum, and so its last bit, differs between the
+// fours of lanes.
 template <int WIDTH>
 __device__ __forceinline__ float lanes_sum(float v) {
     auto moved = [](float x, auto ctrl) {
@@ -73,12 +74,14 @@ __device__ __forceinline__ float lanes_sum(float v) {
     return v;
 }
 
-// Sum over the wave, the same in every lane: the sums of 16 lanes, four of
-// which are read to scalar registers.
+// Sum over the wave, the same in every lane: the sums of 16 lanes, added up
+// along the rows into the last lane and read to a scalar register.
 __device__ __forceinline__ float wave_sum(float v) {
     v = lanes_sum<16>(v);
-    auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
-    return (lane(0) + lane(16)) + (lane(32) + lane(48));
+    // lane 15 of rows 0 and 2 to rows 1 and 3, then lane 31 to rows 2 and 3
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // Has a value computed here: left alone, the compiler moves work behind the
