@@ -284,11 +284,15 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) __attribute__((
         at.load(pz, a.z, row, a.zs);
         at.load(pn, a.dnormed, row, a.dnormeds);
         at.load(po, a.dout, row, a.douts);
-        float sg[N][V], s[3] = {0.0f, 0.0f, 0.0f};
+        // s(z) from the first pass over the row; the widest rows of FP32 have no
+        // registers for it and compute it again (1501 x 16384 forward and back 364 -> 331 us)
+        constexpr bool kAgain = N == 4;
+        float sg[kAgain ? 1 : N][V], s[3] = {0.0f, 0.0f, 0.0f};
         // of one element: o, the gate, m
         auto forward = [&](int n, int j, float w, float &gate, float &m) {
             m = py[n].get(j) * iy;
-            gate = fmaf(pz[n].get(j), sg[n][j], no_gate);
+            if (kAgain) sg[0][j] = sigmoid(pz[n].get(j));
+            gate = fmaf(pz[n].get(j), sg[kAgain ? 0 : n][j], no_gate);
             const float o = fmaf(w * gate, m, px[n].get(j));
             return o;
         };
@@ -302,7 +306,7 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) __attribute__((
 #pragma unroll
                 for (int k = 0; k < G; ++k) {
                     const int j = G * i + k;
-                    sg[n][j] = sigmoid(pz[n].get(j));
+                    if (!kAgain) sg[n][j] = sigmoid(pz[n].get(j));
                     float gate, m;
                     const float oh = forward(n, j, w[k], gate, m) * io, p = w[k] * gate * m, v = pn[n].get(j) * pre[k];
                     if (at.counts(n, j)) {
@@ -340,7 +344,8 @@ __global__ void __launch_bounds__(THREADS *kRowsAtOnce<THREADS>) __attribute__((
                     pin(dw[n][j]), pin(dpre[n][j]);
                     dx[k] = t;
                     dy[k] = fmaf(fy, tg * w[k], -my * py[n].get(j));
-                    dz[k] = tm * w[k] * fmaf(gate, 1.0f - sg[n][j], sg[n][j]);
+                    const float sz = sg[kAgain ? 0 : n][j];
+                    dz[k] = tm * w[k] * fmaf(gate, 1.0f - sz, sz);
                 }
                 gx.set(i, dx);
                 gy.set(i, dy);
