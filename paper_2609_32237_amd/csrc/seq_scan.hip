@@ -114,11 +114,14 @@ __device__ __forceinline__ void look_back(const uint64_t *words, int64_t pitch, 
     for (int j = 0; j < V; ++j) h[j] = __builtin_nanf("");
 }
 
-// Sets the words of the chains to empty and the counters to 0.
+// Sets the words of the chains to empty and the counters to 0, 64 bytes a thread.
+constexpr int kClearAccesses = 4;
 __global__ void __launch_bounds__(256) scan_clear(uint4 *words, int64_t quads, unsigned *counters) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < quads) words[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
-    if (i < kGroups) counters[i * kCounterPitch] = 0u;
+    const int64_t first = (int64_t)blockIdx.x * (256 * kClearAccesses) + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < kClearAccesses; ++k)
+        if (first + 256 * k < quads) words[first + 256 * k] = make_uint4(~0u, ~0u, ~0u, ~0u);
+    if (first < kGroups) counters[first * kCounterPitch] = 0u;
 }
 
 // What a workgroup works on.
@@ -608,9 +611,9 @@ int start(ScanArgs &a, const Cut &c, int type, void *workspace, hipStream_t stre
     a.words = (uint64_t *)workspace;
     a.counters = (unsigned *)((char *)workspace + c.words_bytes());
     void *words = workspace;
-    int64_t quads = (int64_t)(c.words_bytes() / 16);  // at least 64 x 2 words: more than kGroups threads
+    int64_t quads = (int64_t)(c.words_bytes() / 16);
     void *args[] = {&words, &quads, &a.counters};
-    return launch((const void *)scan_clear, dim3((unsigned)ceil_div(quads, 256)), dim3(256), args, 0, stream);
+    return launch((const void *)scan_clear, dim3((unsigned)ceil_div(quads, 256 * kClearAccesses)), dim3(256), args, 0, stream);
 }
 
 bool sizes_ok(int64_t batch, int64_t len, int64_t channels) { return batch >= 0 && len >= 0 && channels >= 1; }
