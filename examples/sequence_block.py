@@ -88,7 +88,7 @@ def forward(w, u, lengths=None, train=False):
         v, r, g, z = _project(h, b["inner"]).chunk(4, -1)
         y, state = scan(v, r, g, b["rate"], None, lengths)
         states.append(state)
-        x, h = norm(x, _project(y, b["outer"]), z.contiguous(), b["post"], b["scale"], b["pre"], eps=EPS)
+        x, h = norm(x, _project(y, b["outer"]), z, b["post"], b["scale"], b["pre"], eps=EPS)
     return _project(h, w["head"])[..., 0], states
 
 

@@ -8,7 +8,7 @@ projection need no copy); weights, states and statistics are contiguous
 float32.  Every function runs on the current stream, or with ``stream=`` (a
 torch stream or a handle) on that one, where its new tensors then belong.
 ``gated_scan_train`` and ``residual_norm_train`` are the same operators as
-autograd functions.
+autograd functions; the others record no gradient.
 """
 from __future__ import annotations
 
@@ -23,9 +23,10 @@ from .torch_api import _raw_device, _stream
 _TYPES = {torch.float32: _l.SEQ_FP32, torch.float16: _l.SEQ_FP16, torch.bfloat16: _l.SEQ_BF16}
 _fp32 = torch.float32
 _new = torch.empty_strided  # with its strides given: 1.3 us, torch.empty 2.1 us
-# sizes alone decide these
+# sizes and strides alone decide these
 _scan_workspace_bytes = functools.lru_cache(maxsize=1024)(_l.lib.seq_scan_workspace_bytes)
 _norm_workspace_bytes = functools.lru_cache(maxsize=1024)(_l.lib.seq_norm_workspace_bytes)
+_host_array = functools.lru_cache(maxsize=1024)(_l.int64s)  # of strides: read only
 
 
 def _type_of(x: torch.Tensor, name: str, dims: int) -> int:
@@ -44,26 +45,32 @@ def _layout(like: torch.Tensor, tensors, names, dims: int):
     """Checks the activations against ``like`` (None: not there); their outer
     strides as a host array, or None where all are contiguous."""
     dtype, shape, device, plain = like.dtype, like.shape, like.get_device(), True
-    for t, name in zip(tensors, names):
+    for t in tensors:
         if t is None:
             continue
-        if t.dtype is not dtype or t.get_device() != device:
-            raise TypeError(f"{name} must have the type and device of the other activations")
-        if t.shape != shape:
-            raise ValueError(f"{name} must have the shape {tuple(shape)}")
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+            _refuse(like, tensors, names)
         plain = plain and t.is_contiguous()
     if plain:
         return None
-    values = []
-    for t, name in zip(tensors, names):
+    values = ()
+    for k, t in enumerate(tensors):
         if t is None:
             values += (0,) * dims
             continue
         strides = t.stride()
         if strides[-1] != 1 and shape[-1] > 1:
-            raise ValueError(f"the last axis of {name} must be consecutive in memory")
+            raise ValueError(f"the last axis of {names[k]} must be consecutive in memory")
         values += strides[:dims]
-    return _l.int64s(values)
+    return _host_array(values)
+
+
+def _refuse(like, tensors, names):
+    for t, name in zip(tensors, names):
+        if t is not None and (t.dtype is not like.dtype or t.get_device() != like.get_device()):
+            raise TypeError(f"{name} must have the type and device of the other activations")
+        if t is not None and t.shape != like.shape:
+            raise ValueError(f"{name} must have the shape {tuple(like.shape)}")
 
 
 def _weight(t, name: str, shape, like: torch.Tensor, dtype=_fp32):
@@ -92,20 +99,10 @@ def _workspace(nbytes: int, given, like: torch.Tensor):
     return given, given.data_ptr()
 
 
-def _on_its_stream(call):
-    """``stream=``: the call as if that stream were the current one, so that new
-    memory comes from its pool too (the current stream's may still be in use there)."""
-
-    @functools.wraps(call)
-    def on_stream(*args, stream=None, **kwargs):
-        if stream is None:
-            return call(*args, **kwargs)
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream))
-        with torch.cuda.stream(stream):
-            return call(*args, **kwargs)
-
-    return on_stream
+def _on(stream):
+    """A context that makes ``stream`` the current one, so that new memory comes from its
+    pool too (the current stream's may still be in use there)."""
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
 
 
 def gated_scan_saved(x: torch.Tensor) -> torch.Tensor:
@@ -115,8 +112,8 @@ def gated_scan_saved(x: torch.Tensor) -> torch.Tensor:
     return _new((b, n, d), (n * d, d, 1), dtype=_fp32, device=x.device)
 
 
-@_on_its_stream
-def gated_scan(x, r, g, rate, state=None, lengths=None, *, out=None, state_out=None, saved=None, workspace=None):
+def gated_scan(x, r, g, rate, state=None, lengths=None, *, out=None, state_out=None, saved=None, workspace=None,
+               stream=None):
     """The gated linear recurrence of each channel of (batch, tokens, channels):
 
         h_t = h_(t-1) + q_t (c_t - h_(t-1)),  q_t = rate sigmoid(r_t),  c_t = sigmoid(g_t) x_t
@@ -127,6 +124,9 @@ def gated_scan(x, r, g, rate, state=None, lengths=None, *, out=None, state_out=N
     those behind leave the state and give 0.  ``saved`` (``gated_scan_saved``)
     is filled for ``gated_scan_backward``.
     """
+    if stream is not None:
+        with _on(stream):
+            return gated_scan(x, r, g, rate, state, lengths, out=out, state_out=state_out, saved=saved, workspace=workspace)
     kind = _type_of(x, "x", 3)
     b, t, d = x.shape
     if out is None:
@@ -148,30 +148,35 @@ def gated_scan(x, r, g, rate, state=None, lengths=None, *, out=None, state_out=N
     return out, state_out
 
 
-@_on_its_stream
-def gated_scan_step(x, r, g, rate, state, *, out=None):
+def gated_scan_step(x, r, g, rate, state, *, out=None, stream=None):
     """One token (batch, channels) of ``gated_scan``; ``state`` is updated in place.  Returns y."""
     if x.dim() != 2 or r.dim() != 2 or g.dim() != 2:
         raise ValueError("x, r and g must have 2 axes")
     y, _ = gated_scan(x.unsqueeze(1), r.unsqueeze(1), g.unsqueeze(1), rate, state,
-                      out=None if out is None else out.unsqueeze(1), state_out=state)
+                      out=None if out is None else out.unsqueeze(1), state_out=state, stream=stream)
     return y.squeeze(1) if out is None else out
 
 
-@_on_its_stream
 def gated_scan_backward(grad_out, x, r, g, rate, saved, lengths=None, *, grad_state=None, out=(None, None, None),
-                        workspace=None):
+                        workspace=None, stream=None):
     """Gradient of ``gated_scan``: (dx, dr, dg, drate, dstate) from the
     gradients of y and of the state after the last token (None: zeros).
     ``out``: tensors for dx, dr and dg, slices of one buffer for example."""
+    if stream is not None:
+        with _on(stream):
+            return gated_scan_backward(grad_out, x, r, g, rate, saved, lengths, grad_state=grad_state, out=out, workspace=workspace)
     kind = _type_of(x, "x", 3)
     b, t, d = x.shape
-    dx, dr, dg = (_new((b, t, d), (t * d, d, 1), dtype=x.dtype, device=x.device) if v is None else v for v in out)
+    dx, dr, dg = out
+    dtype, device, plain = x.dtype, x.device, (t * d, d, 1)
+    dx = _new((b, t, d), plain, dtype=dtype, device=device) if dx is None else dx
+    dr = _new((b, t, d), plain, dtype=dtype, device=device) if dr is None else dr
+    dg = _new((b, t, d), plain, dtype=dtype, device=device) if dg is None else dg
     strides = _layout(x, (grad_out, x, r, g, dx, dr, dg), ("grad_out", "x", "r", "g", "dx", "dr", "dg"), 2)
     if rate is None or saved is None:
         raise TypeError("rate or saved is missing")
-    drate = _new((d,), (1,), dtype=_fp32, device=x.device)
-    dstate = _new((b, d), (d, 1), dtype=_fp32, device=x.device)
+    drate = _new((d,), (1,), dtype=_fp32, device=device)
+    dstate = _new((b, d), (d, 1), dtype=_fp32, device=device)
     _, ws = _workspace(_scan_workspace_bytes(b, t, d, kind, 1), workspace, x)
     _l.check(_l.lib.seq_scan_backward(
         b, t, d, kind, grad_out.data_ptr(), x.data_ptr(), r.data_ptr(), g.data_ptr(),
@@ -189,8 +194,8 @@ def residual_norm_stats(x: torch.Tensor) -> torch.Tensor:
     return torch.empty((*x.shape[:-1], 2), dtype=_fp32, device=x.device)
 
 
-@_on_its_stream
-def residual_norm(x, y=None, z=None, post=None, scale=None, pre=None, *, eps: float, out=None, normed=None, stats=None):
+def residual_norm(x, y=None, z=None, post=None, scale=None, pre=None, *, eps: float, out=None, normed=None, stats=None,
+                  stream=None):
     """The end of a block and the beginning of the next one, over the last axis:
 
         o = x + scale post (y / rms(y)) silu(z),  n = pre o / rms(o)
@@ -200,6 +205,9 @@ def residual_norm(x, y=None, z=None, post=None, scale=None, pre=None, *, eps: fl
     None.  ``stats`` (``residual_norm_stats``) is filled for
     ``residual_norm_backward``.
     """
+    if stream is not None:
+        with _on(stream):
+            return residual_norm(x, y, z, post, scale, pre, eps=eps, out=out, normed=normed, stats=stats)
     if x.dim() != 2:  # as rows, without a copy
         shape, part = x.shape, [v if v is None else v.view(-1, v.shape[-1]) for v in (x, y, z, out, normed)]
         o2, n2 = residual_norm(*part[:3], post, scale, pre, eps=eps, out=part[3], normed=part[4],
@@ -220,25 +228,30 @@ def residual_norm(x, y=None, z=None, post=None, scale=None, pre=None, *, eps: fl
     return x if y is None else out, normed
 
 
-@_on_its_stream
 def residual_norm_backward(grad_out, grad_normed, x, y, z, post, scale, pre, stats, *, eps: float,
-                           out=(None, None, None), workspace=None):
+                           out=(None, None, None), workspace=None, stream=None):
     """Gradient of ``residual_norm``: (dx, dy, dz, dpost, dscale, dpre), None
     where the argument is.  ``grad_out`` may be None (zeros), ``grad_normed``
     is None where ``pre`` is.  ``out``: tensors for dx, dy and dz."""
+    if stream is not None:
+        with _on(stream):
+            return residual_norm_backward(grad_out, grad_normed, x, y, z, post, scale, pre, stats, eps=eps, out=out, workspace=workspace)
     if x.dim() != 2:
         shape, part = x.shape, [v if v is None else v.view(-1, v.shape[-1]) for v in (grad_out, grad_normed, x, y, z, *out)]
         found = residual_norm_backward(*part[:5], post, scale, pre, stats.view(-1, 2), eps=eps, out=part[5:], workspace=workspace)
         return tuple(v if v is None else v.view(shape) if given is None else given for v, given in zip(found, out)) + found[3:]
     kind = _type_of(x, "x", 2)
     rows, d = x.shape
-    dx, dy, dz = (_new((rows, d), (d, 1), dtype=x.dtype, device=x.device) if v is None and of is not None else v
-                  for v, of in zip(out, (x, y, z)))
+    dx, dy, dz = out
+    dtype, device = x.dtype, x.device
+    dx = _new((rows, d), (d, 1), dtype=dtype, device=device) if dx is None else dx
+    dy = _new((rows, d), (d, 1), dtype=dtype, device=device) if dy is None and y is not None else dy
+    dz = _new((rows, d), (d, 1), dtype=dtype, device=device) if dz is None and z is not None else dz
     strides = _layout(x, (grad_out, grad_normed, x, y, z, dx, dy, dz),
                       ("grad_out", "grad_normed", "x", "y", "z", "dx", "dy", "dz"), 1)
     if stats is None:
         raise TypeError("stats is missing")
-    grads = [None if w is None else _new((d,), (1,), dtype=_fp32, device=x.device) for w in (post, scale, pre)]
+    grads = [None if w is None else _new((d,), (1,), dtype=_fp32, device=device) for w in (post, scale, pre)]
     _, ws = _workspace(_norm_workspace_bytes(rows, d, kind), workspace, x)
     _l.check(_l.lib.seq_norm_backward(
         rows, d, kind, _ptr(grad_out), _ptr(grad_normed), x.data_ptr(), _ptr(y), _ptr(z), strides,
@@ -258,6 +271,7 @@ class _GatedScan(torch.autograd.Function):
         return y, last
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_y, grad_last):
         x, r, g, rate, saved, lengths = ctx.saved_tensors
         grad_y = torch.zeros_like(x) if grad_y is None else grad_y if grad_y.stride(-1) == 1 else grad_y.contiguous()
@@ -278,6 +292,7 @@ class _ResidualNorm(torch.autograd.Function):
         return (normed,) if y is None else (out, normed) if pre is not None else (out,)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, *grads):
         x, y, z, post, scale, pre, stats = ctx.saved_tensors
         grad_out, grad_normed = None if y is None else grads[0], None if pre is None else grads[-1]
