@@ -113,7 +113,7 @@ struct Pack {
     __device__ __forceinline__ void load(const T *p) { u = ((const Unaligned *)p)->u; }
     __device__ __forceinline__ void store(T *p) const { ((Unaligned *)p)->u = u; }
     // `past`: past the caches, for results too large to be found there again
-    __device__ __forceinline__ void store(T *p, bool past) const {
+    __device__ __forceinline__ void store_past(T *p, bool past) const {
         if (past)
             __builtin_nontemporal_store(u, &((Unaligned *)p)->u);
         else
@@ -126,7 +126,7 @@ struct Pack {
     // an unsigned 32-bit offset of bytes from it needs no 64-bit address in vector
     // registers.
     __device__ __forceinline__ void load(const T *row, unsigned at) { load((const T *)((const char *)row + at * (unsigned)sizeof(T))); }
-    __device__ __forceinline__ void store(T *row, unsigned at, bool past) const { store((T *)((char *)row + at * (unsigned)sizeof(T)), past); }
+    __device__ __forceinline__ void store(T *row, unsigned at) const { store((T *)((char *)row + at * (unsigned)sizeof(T))); }
     // The same of a row of `end` elements, zeros behind it.  WHOLE: `end` is a multiple of V.
     template <bool WHOLE>
     __device__ __forceinline__ void load(const T *row, unsigned at, unsigned end) {
@@ -143,9 +143,9 @@ struct Pack {
         }
     }
     template <bool WHOLE>
-    __device__ __forceinline__ void store(T *row, unsigned at, unsigned end, bool past) const {
+    __device__ __forceinline__ void store(T *row, unsigned at, unsigned end) const {
         if (WHOLE ? at < end : at + V <= end) {
-            store(row, at, past);
+            store(row, at);
         } else if (!WHOLE) {
             T v[V];
             __builtin_memcpy(v, &u, sizeof(u));
