@@ -518,6 +518,8 @@ struct Shape {
         return groups <= most ? groups : ceil_div(groups, ceil_div(groups, most));
     }
     int64_t parts(int64_t rows) const { return backward_grid(rows) * at_once(); }
+    // As many as stay on the CUs together: 16384 x 4096 in bf16 forward and back 342 us
+    // with 512 of them, with 768 395 us, with 1024 352 us.
     int64_t backward_grid(int64_t rows) const { return grid(rows, threads <= 256 ? 1024 : threads == 512 ? 512 : 256); }
     int64_t forward_grid(int64_t rows) const { return grid(rows, threads <= 256 ? 2048 : threads == 512 ? 1024 : 512); }
 };

@@ -201,6 +201,21 @@ def test_in_place_with_odd_widths(sq, dtype, rows, d):
     assert all(torch.equal(a, b) for a, b in zip(got, grads))
 
 
+@pytest.mark.parametrize("rows, d", [(40, 4099), (300, 1001), (200, 2055), (60, 8191), (20, 16383)])
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_shared_channels_have_one_value(sq, dtype, rows, d):
+    """Where two lanes work out the same channel of an odd width, it must not matter which
+    of them writes last: many runs, the same bits."""
+    (x, y, z, go, gn), w = inputs(rows, d, dtype, 16)
+    first = None
+    for _ in range(25):
+        stats = sq.residual_norm_stats(x)
+        out = [*sq.residual_norm(x, y, z, *w, eps=EPS, stats=stats)]
+        out += sq.residual_norm_backward(go, gn, x, y, z, *w, stats, eps=EPS)
+        first = first or out
+        assert all(torch.equal(a, b) for a, b in zip(first, out))
+
+
 @pytest.mark.parametrize("d", [3, 100, 515, 1024, 20000])
 def test_writes_nothing_outside(sq, d):
     """Outputs inside wider buffers: what surrounds them keeps its values."""
