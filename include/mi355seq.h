@@ -63,8 +63,10 @@ enum { SEQ_SCAN_CHUNK = 16 };
  *
  *   batch, len   sequences (>= 0) and tokens of each (>= 0); len = 1 is the
  *                single-token step of a server.
- *   channels     >= 1.  batch, len and channels are at most 2^31 - 1, their
- *                product at most 2^40 (else SEQ_EUNSUPPORTED).
+ *   channels     >= 1.  batch, len and channels are at most 2^31 - 1, and one
+ *                launch of 2^32 threads has to hold the call: 512 for each
+ *                128 tokens of 64 channels of a sequence, 64 to 512 where it
+ *                has fewer tokens (else SEQ_EUNSUPPORTED).
  *   type         SEQ_FP32, SEQ_FP16 or SEQ_BF16: x, r, g and y.
  *   x, r, g      inputs (batch, len, channels).
  *   strides      host array of 8: batch and token stride of x, r, g, y; NULL:

@@ -67,10 +67,10 @@ __device__ __forceinline__ float lanes_sum(float v) {
     auto moved = [](float x, auto ctrl) {
         return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
     };
-    v += moved(v, std::integral_constant<int, 0xb1>{});                         // lanes 1 0 3 2 of each four
-    v += moved(v, std::integral_constant<int, 0x4e>{});                         // lanes 2 3 0 1
-    if (WIDTH > 4) v += moved(v, std::integral_constant<int, 0x124>{});   // rotated by 4 within 16
-    if (WIDTH > 8) v += moved(v, std::integral_constant<int, 0x128>{});   // rotated by 8
+    v += moved(v, std::integral_constant<int, 0xb1>{});  // lanes 1 0 3 2 of each four
+    v += moved(v, std::integral_constant<int, 0x4e>{});  // lanes 2 3 0 1
+    if (WIDTH > 4) v += moved(v, std::integral_constant<int, 0x124>{});  // rotated by 4 within 16
+    if (WIDTH > 8) v += moved(v, std::integral_constant<int, 0x128>{});  // rotated by 8
     return v;
 }
 

@@ -14,6 +14,7 @@ namespace mi355seq {
 
 constexpr int64_t kMaxSize = 0x7fffffff;
 constexpr int64_t kMaxElements = int64_t(1) << 40;
+constexpr int64_t kMaxThreads = 0xffffffff;  // of one launch
 
 inline size_t element_bytes(int type) { return type == SEQ_FP32 ? 4 : 2; }
 inline bool known_type(int type) { return type == SEQ_FP32 || type == SEQ_FP16 || type == SEQ_BF16; }

@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(kSumChannels *kSumGroups) norm_sum(NormArgs a,
 
 // Rows wider than a workgroup holds are read once for each sum and once more
 // for the results, which are written after their row's last read.
-constexpr int kWideThreads = 1024, kWideGroups = 64;
+constexpr int kWideThreads = 1024, kWideGroups = 64, kWideForward = 4096;  // workgroups of the gradient and of the forward pass, at most
 
 template <typename E>
 struct Wide {
@@ -439,28 +439,30 @@ template <typename E>
 __global__ void __launch_bounds__(kWideThreads) norm_forward_wide(NormArgs a) {
     __shared__ float buffers[2][1][kWideThreads / kWave];
     GroupSum<kWideThreads, 1> sum{buffers};
-    const Wide<E> row{a, blockIdx.x};
-    float iy = 0.0f, io = 0.0f, s[1] = {0.0f};
-    if (a.y) {
-        for (int d = threadIdx.x; d < a.channels; d += kWideThreads) s[0] = fmaf(row.at(a.y, a.ys, d), row.at(a.y, a.ys, d), s[0]);
-        sum(s);
-        iy = inverse_rms(a, s[0]);
-    }
-    if (a.pre) {
-        s[0] = 0.0f;
-        for (int d = threadIdx.x; d < a.channels; d += kWideThreads) {
-            const float v = row.o(d, iy);
-            s[0] = fmaf(v, v, s[0]);
+    for (int64_t k = blockIdx.x; k < a.rows; k += gridDim.x) {
+        const Wide<E> row{a, k};
+        float iy = 0.0f, io = 0.0f, s[1] = {0.0f};
+        if (a.y) {
+            for (int d = threadIdx.x; d < a.channels; d += kWideThreads) s[0] = fmaf(row.at(a.y, a.ys, d), row.at(a.y, a.ys, d), s[0]);
+            sum(s);
+            iy = inverse_rms(a, s[0]);
         }
-        sum(s);
-        io = inverse_rms(a, s[0]);
+        if (a.pre) {
+            s[0] = 0.0f;
+            for (int d = threadIdx.x; d < a.channels; d += kWideThreads) {
+                const float v = row.o(d, iy);
+                s[0] = fmaf(v, v, s[0]);
+            }
+            sum(s);
+            io = inverse_rms(a, s[0]);
+        }
+        for (int d = threadIdx.x; d < a.channels; d += kWideThreads) {
+            const float o = row.o(d, iy);
+            if (a.out) row.put(a.out, a.outs, d, o);
+            if (a.pre) row.put(a.normed, a.normeds, d, o * io * a.pre[d]);
+        }
+        if (a.stats && threadIdx.x < 2) a.stats[2 * k + threadIdx.x] = threadIdx.x ? io : iy;
     }
-    for (int d = threadIdx.x; d < a.channels; d += kWideThreads) {
-        const float o = row.o(d, iy);
-        if (a.out) row.put(a.out, a.outs, d, o);
-        if (a.pre) row.put(a.normed, a.normeds, d, o * io * a.pre[d]);
-    }
-    if (a.stats && threadIdx.x < 2) a.stats[2 * row.row + threadIdx.x] = threadIdx.x ? io : iy;
 }
 
 // A workgroup's rows one after another; its sums for the weights' gradients are
@@ -617,7 +619,7 @@ int seq_norm_forward(int64_t rows, int64_t channels, int type, const void *x, co
     a.post = post, a.scale = scale, a.pre = pre, a.stats = stats;
     void *args[] = {&a};
     const Shape s = shape_of(channels, type);
-    const int64_t groups = s.accesses ? s.forward_grid(rows) : rows;
+    const int64_t groups = s.accesses ? s.forward_grid(rows) : s.grid(rows, kWideForward);
     return launch(kernel_of<false>(s, channels, type), dim3((unsigned)groups), dim3(s.threads * s.at_once()), args, s.lds(type), stream);
 }
 

@@ -625,7 +625,9 @@ bool sizes_ok(int64_t batch, int64_t len, int64_t channels) { return batch >= 0 
 bool sizes_supported(int64_t batch, int64_t len, int64_t channels) {
     if (batch > kMaxSize || len > kMaxSize || channels > kMaxSize) return false;
     const __int128 n = (__int128)batch * (len > 0 ? len : 1) * channels;
-    return n <= kMaxElements && cut_of(batch, len, channels, SEQ_FP32, true).grid() <= kMaxSize;
+    if (n > kMaxElements) return false;
+    const Cut c = cut_of(batch, len, channels, SEQ_FP32, true);  // the finest
+    return c.grid() <= kMaxThreads / (kWave * c.waves);
 }
 
 }  // namespace
@@ -693,7 +695,7 @@ int seq_scan_forward(int64_t batch, int64_t len, int64_t channels, int type, con
     const int rc = start(a, c, type, workspace, stream);
     if (rc != SEQ_OK) return rc;
     const int64_t per_row = ceil_div(channels, kStepChannels), items = batch * per_row;
-    if (len == 1 && items <= kMaxSize) {
+    if (len == 1 && items <= kMaxSize && channels < (int64_t(1) << 30)) {  // 32-bit offsets of bytes in a row
         unsigned row = (unsigned)per_row, all = (unsigned)items;
         void *args[] = {&a, &row, &all};
         const void *kernel = type == SEQ_FP32 ? step_kernel<F32>(channels) : type == SEQ_FP16 ? step_kernel<F16>(channels) : step_kernel<BF16>(channels);

@@ -80,6 +80,7 @@ PLAIN = [ROW, 64] * 4
     (dict(batch=-1), "SEQ_EINVAL"), (dict(len=-1), "SEQ_EINVAL"), (dict(channels=0), "SEQ_EINVAL"), (dict(type=3), "SEQ_EINVAL"),
     (dict(type=-1), "SEQ_EINVAL"), (dict(batch=1 << 31), "SEQ_EUNSUPPORTED"), (dict(len=1 << 31), "SEQ_EUNSUPPORTED"),
     (dict(len=1 << 30, channels=1 << 12), "SEQ_EUNSUPPORTED"),
+    (dict(batch=20_000_000, len=100, channels=1), "SEQ_EUNSUPPORTED"),  # more threads than one launch holds
     (dict(x=None), "SEQ_EINVAL"), (dict(r=None), "SEQ_EINVAL"), (dict(g=None), "SEQ_EINVAL"), (dict(rate=None), "SEQ_EINVAL"),
     (dict(y=None), "SEQ_EINVAL"),
     (dict(x=P + 1), "SEQ_EALIGN"), (dict(rate=P + 2), "SEQ_EALIGN"), (dict(state_out=P + 6 * GAP + 2), "SEQ_EALIGN"),

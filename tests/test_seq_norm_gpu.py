@@ -81,7 +81,7 @@ def test_widths(sq, dtype, d):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
-@pytest.mark.parametrize("rows, d", [(1, 512), (2, 100), (77, 96), (1000, 64), (2053, 33), (600, 2048), (5000, 256), (700, 5000)])
+@pytest.mark.parametrize("rows, d", [(1, 512), (2, 100), (77, 96), (1000, 64), (2053, 33), (600, 2048), (5000, 256), (700, 5000), (4200, 16400)])
 def test_rows(sq, dtype, rows, d):
     one(sq, rows, d, dtype, seed=rows)
 
